@@ -30,6 +30,7 @@ extern "C" {
 typedef struct dllmc_ctx dllmc_ctx; /* opaque host object */
 
 enum { DLLMC_F32 = 0, DLLMC_BF16 = 1 };
+enum { DLLMC_KV4 = 2 }; /* a cache tensor in 4 bits: a cache_format of the operations below, never a dtype */
 
 enum {
   DLLMC_OK = 0,
@@ -382,6 +383,81 @@ size_t dllmc_op_attention_scratch_bytes(void);
 int dllmc_op_attention(int32_t dtype, const void* q, int32_t B, int32_t Mq, const void* k_cache,
                        const void* v_cache, int32_t n, int32_t H_q, int32_t H_kv, int32_t d_h,
                        void* out, float* scratch, void* hip_stream);
+
+/* ---- the step's pieces in fewer bits -------------------------------------------------------
+ * The paper's Limitations paragraph names the growth of the caches with the sequence length as its open problem.  Below: K and
+ * V held in 4 bits and the attention that reads them, the attention weight that cached positions accumulate and the
+ * eviction of positions by it, and linear maps in 8-bit integers, whose weights are half the bytes an adaptive step streams.
+ * As with the other single operations all memory is the caller's, nothing is allocated, cleared by the runtime or
+ * waited for (every call can be captured into a graph), and calls that share scratch must be ordered.  Results must lie
+ * apart from the operands (DLLMC_EINVAL) unless said otherwise.  Data pointers are 16-byte aligned, int32 and float32 lists 4-byte.
+ *
+ * 4-bit cache tensor of cache_rows rows, H heads of d_h elements (d_h a multiple of 32, H * d_h <= 65536): dllmc_kv4_bytes()
+ * bytes (0: invalid).  Codes [H][cache_rows][d_h / 2], element 2t of a row in the low half of byte t; at the next multiple of
+ * 256 bytes scale bytes [H][cache_rows][d_h / 32].  A block of 32 elements has one scale s that stands for 2^(s - 127): the
+ * smallest power of two, of 2^-125 .. 2^125, with max |x| <= 6 * 2^(s - 127).  A code is a sign and the index of one of 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6, the nearest to x / 2^(s - 127) (ties to the even index, beyond 6: 6).  s = 255: the block held an infinity
+ * or NaN and all of it reads as NaN. */
+size_t dllmc_kv4_bytes(int32_t cache_rows, int32_t H, int32_t d_h);
+/* Row rows[i] (i if rows is NULL) of the tensor <- row i of x [M, H * d_h], i < M; entries outside [0, cache_rows) are
+ * left out.  A row must not be listed twice (which of the two is kept is undefined then). */
+int dllmc_op_kv4_store(int32_t dtype, const void* x, int32_t M, const int32_t* rows, void* cache, int32_t cache_rows,
+                       int32_t H, int32_t d_h, void* hip_stream);
+/* out [M, H * d_h] row i = the values of row rows[i] (i if NULL), exact in either dtype; zeros where rows[i] is no row. */
+int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int32_t H, int32_t d_h, const int32_t* rows,
+                      int32_t M, void* out, void* hip_stream);
+
+/* Cached keys of the operations below: sequence b has the positions j < lens[b] (n if lens is NULL; values outside [0, n] count
+ * as the nearest of the two), position j in cache row row_map[b * n + j] (b * n + j if row_map is NULL).  A position whose entry is
+ * no row of the cache is not there.  What lies in rows and positions that are not there has no influence whatever it
+ * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements.
+ *
+ * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
+ * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without
+ * keys gets zeros and an lse of minus infinity.  scratch: at least dllmc_op_attention_kv4_scratch_bytes() bytes, which may
+ * be 0. */
+size_t dllmc_op_attention_kv4_scratch_bytes(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv,
+                                            int32_t d_h);
+int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, const void* k_cache, const void* v_cache,
+                           int32_t cache_rows, const int32_t* row_map, const int32_t* lens, int32_t n, int32_t H_q,
+                           int32_t H_kv, int32_t d_h, void* out, float* lse, void* scratch, size_t scratch_bytes,
+                           void* hip_stream);
+/* Attention weight of every cached position: acc_out[b][j] = acc_in[b][j] (0 if NULL; may be acc_out) + the sum over the Mq
+ * queries and H_q heads of their softmax probabilities, float32 [B, n]; positions that are not there get nothing.  k_cache:
+ * [cache_rows, H_kv * d_h] in the dtype of q (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what
+ * dllmc_op_attention_kv4 gave for these operands, or NULL (then the keys are read twice).  Bit-reproducible. */
+size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n,
+                                                int32_t H_q, int32_t H_kv, int32_t d_h);
+int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* q, int32_t B, int32_t Mq,
+                               const void* k_cache, int32_t cache_rows, const int32_t* row_map, const int32_t* lens,
+                               int32_t n, int32_t H_q, int32_t H_kv, int32_t d_h, const float* lse, const float* acc_in,
+                               float* acc_out, void* scratch, size_t scratch_bytes, void* hip_stream);
+/* Positions that stay when every sequence may keep `keep` of its n: the first `first` and the last `last` of its lens[b]
+ * (first + last <= keep), then those of the largest acc [B, n], equal ones lowest position first (NaN counts as less than
+ * anything).  kept [B, keep]: the positions, ascending; kept_rows: their cache rows; new_lens[b]: how many, the smaller of
+ * keep and what is there; acc_out (may be NULL): their weights.  Behind them kept and kept_rows are -1, acc_out 0. */
+int dllmc_op_evict(const float* acc, int32_t B, int32_t n, const int32_t* lens, const int32_t* row_map, int32_t cache_rows,
+                   int32_t keep, int32_t first, int32_t last, int32_t* kept, int32_t* kept_rows, int32_t* new_lens,
+                   float* acc_out, void* hip_stream);
+/* Rows moved together: row i of k_dst (and of v_dst, both of dst_rows >= M rows) = row rows[i] of k_src (v_src) of src_rows
+ * rows, i < M; where rows[i] is no row, row i is left as it was.  cache_format DLLMC_F32 or DLLMC_BF16: tensors [rows, H * d_h],
+ * any d_h; DLLMC_KV4: 4-bit ones.  v_src and v_dst may both be NULL. */
+int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32_t src_rows, int32_t dst_rows, int32_t H,
+                     int32_t d_h, const void* k_src, void* k_dst, const void* v_src, void* v_dst, void* hip_stream);
+
+/* Rows in 8-bit integers: dllmc_i8_row_bytes(K) bytes each, K rounded up to 128 (K <= 131072; 0: invalid), zeros behind the K-th.
+ * q[i][k] = the integer nearest to the float32 product x[r][k] * (127 / max|x[r]|), ties to even, scale[i] = max|x[r]| / 127, r =
+ * row_idx[i] (i if NULL).  A row whose maximum is below 2^-118 becomes zeros with scale 0, one with an infinity or NaN zeros with
+ * scale NaN.  For weights (rows = output channels) as for activations (rows = tokens). */
+size_t dllmc_i8_row_bytes(int32_t K);
+int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
+                    void* hip_stream);
+/* out[i][j] = a_scale[i] * w_scale[j] * (sum over k of a[i][k] * w[j][k], in integers), [M, N] of dtype; a and w as dllmc_op_quant8
+ * leaves them.  scratch: at least dllmc_op_linear_i8_scratch_bytes() bytes, which may be 0.  Bit-reproducible. */
+size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K);
+int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int32_t M, const int8_t* w,
+                       const float* w_scale, int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes,
+                       void* hip_stream);
 
 /* ---- achievable-peak probes (measurement aids, not steps of the method) ----
  * What this GPU delivers for the plainest kernels of each kind, so that a roofline fraction

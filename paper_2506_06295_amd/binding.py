@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdllmc.so")
 
 DLLMC_F32, DLLMC_BF16 = 0, 1
+DLLMC_KV4 = 2
 _DTYPES = {"f32": (DLLMC_F32, torch.float32), "bf16": (DLLMC_BF16, torch.bfloat16)}
 _ERR = {-1: "EINVAL", -2: "ESTATE", -3: "EHIP", -4: "ENOMEM", -5: "ETOOBIG"}
 
@@ -32,6 +33,9 @@ EXPORTS = (
     "dllmc_op_linear_static", "dllmc_op_linear_static_max_elements", "dllmc_op_linear_rows",
     "dllmc_pool_bytes", "dllmc_workspace_bytes_paged", "dllmc_create_paged", "dllmc_set_page_table",
     "dllmc_pool_create", "dllmc_pool_available", "dllmc_pool_alloc", "dllmc_pool_free", "dllmc_pool_destroy",
+    "dllmc_kv4_bytes", "dllmc_op_kv4_store", "dllmc_op_kv4_load", "dllmc_op_attention_kv4_scratch_bytes",
+    "dllmc_op_attention_kv4", "dllmc_op_attention_weights_scratch_bytes", "dllmc_op_attention_weights", "dllmc_op_evict",
+    "dllmc_op_compact", "dllmc_i8_row_bytes", "dllmc_op_quant8", "dllmc_op_linear_i8_scratch_bytes", "dllmc_op_linear_i8",
 )
 NUM_KERNEL_CLASSES = 13
 
@@ -189,6 +193,25 @@ def lib() -> C.CDLL:
         L.dllmc_probe_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.dllmc_probe_mfma.restype = C.c_int
         L.dllmc_probe_mfma.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.POINTER(C.c_double), C.c_void_p]
+        i32, ptr, size = C.c_int32, C.c_void_p, C.c_size_t
+        for name, res, args in (
+                ("dllmc_kv4_bytes", size, [i32] * 3),
+                ("dllmc_op_kv4_store", C.c_int, [i32, ptr, i32, ptr, ptr, i32, i32, i32, ptr]),
+                ("dllmc_op_kv4_load", C.c_int, [i32, ptr, i32, i32, i32, ptr, i32, ptr, ptr]),
+                ("dllmc_op_attention_kv4_scratch_bytes", size, [i32] * 7),
+                ("dllmc_op_attention_kv4", C.c_int, [i32, ptr, i32, i32, ptr, ptr, i32, ptr, ptr, i32, i32, i32, i32, ptr, ptr,
+                                                     ptr, size, ptr]),
+                ("dllmc_op_attention_weights_scratch_bytes", size, [i32] * 8),
+                ("dllmc_op_attention_weights", C.c_int, [i32, i32, ptr, i32, i32, ptr, i32, ptr, ptr, i32, i32, i32, i32, ptr,
+                                                         ptr, ptr, ptr, size, ptr]),
+                ("dllmc_op_evict", C.c_int, [ptr, i32, i32, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr, ptr, ptr]),
+                ("dllmc_op_compact", C.c_int, [i32, ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, ptr]),
+                ("dllmc_i8_row_bytes", size, [i32]),
+                ("dllmc_op_quant8", C.c_int, [i32, ptr, ptr, i32, i32, ptr, ptr, ptr]),
+                ("dllmc_op_linear_i8_scratch_bytes", size, [i32] * 3),
+                ("dllmc_op_linear_i8", C.c_int, [i32, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, size, ptr])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, args
         _lib = L
     return _lib
 
@@ -520,6 +543,170 @@ def op_attention(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     _check(lib().dllmc_op_attention(_DTYPES[dtype][0], q.data_ptr(), B, Mq, k_cache.data_ptr(),
                                     v_cache.data_ptr(), n, H_q, H_kv, d_h, out.data_ptr(),
                                     _ptr(scratch), _stream_handle()), "dllmc_op_attention")
+    return out
+
+
+# ---- the step's pieces in fewer bits ------------------------------------------------------------
+def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
+    """Address of a contiguous tensor of the current device, this dtype and shape (None stays None)."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.device.index == torch.cuda.current_device() and t.is_contiguous() and t.dtype == dtype
+            and tuple(t.shape) == tuple(shape)):
+        raise DllmcError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
+
+
+def _scratch(nbytes: int) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+def _need_cache(name: str, fmt: str, t: torch.Tensor, cache_rows: int, H: int, d_h: int) -> int:
+    if fmt == "kv4":
+        return _need(name, t, torch.uint8, (kv4_bytes(cache_rows, H, d_h),))
+    return _need(name, t, _DTYPES[fmt][1], (cache_rows, H * d_h))
+
+
+def _format(fmt: str) -> int:
+    return DLLMC_KV4 if fmt == "kv4" else _DTYPES[fmt][0]
+
+
+def kv4_bytes(cache_rows: int, H: int, d_h: int) -> int:
+    """Bytes of a 4-bit cache tensor (a uint8 tensor of that size holds it)."""
+    n = lib().dllmc_kv4_bytes(cache_rows, H, d_h)
+    if n == 0:
+        raise DllmcError(f"dllmc_kv4_bytes: no 4-bit tensor of {cache_rows} rows, {H} heads of {d_h}")
+    return n
+
+
+def op_kv4_store(dtype: str, x: torch.Tensor, cache: torch.Tensor, cache_rows: int, H: int, d_h: int,
+                 rows: Optional[torch.Tensor] = None) -> None:
+    """Rows of x [M, H * d_h] into rows `rows` (int32 [M], distinct; 0 .. M - 1 if None) of a 4-bit cache tensor."""
+    M = x.shape[0]
+    code, tdt = _DTYPES[dtype]
+    _check(lib().dllmc_op_kv4_store(code, _need("x", x, tdt, (M, H * d_h)), M, _need("rows", rows, torch.int32, (M,)),
+                                    _need_cache("cache", "kv4", cache, cache_rows, H, d_h), cache_rows, H, d_h,
+                                    _stream_handle()), "dllmc_op_kv4_store")
+
+
+def op_kv4_load(dtype: str, cache: torch.Tensor, cache_rows: int, H: int, d_h: int,
+                rows: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """[M, H * d_h]: the values of rows `rows` (int32 [M]; all if None) of a 4-bit cache tensor."""
+    M = cache_rows if rows is None else rows.numel()
+    code, tdt = _DTYPES[dtype]
+    at = _need_cache("cache", "kv4", cache, cache_rows, H, d_h)
+    out = torch.empty((M, H * d_h), dtype=tdt, device="cuda")
+    _check(lib().dllmc_op_kv4_load(code, at, cache_rows, H, d_h, _need("rows", rows, torch.int32, (M,)), M, out.data_ptr(),
+                                   _stream_handle()), "dllmc_op_kv4_load")
+    return out
+
+
+def op_attention_kv4(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, cache_rows: int, n: int,
+                     H_q: int, H_kv: int, d_h: int, lens: Optional[torch.Tensor] = None,
+                     row_map: Optional[torch.Tensor] = None, with_lse: bool = False):
+    """Attention rows [B, Mq, H_q * d_h] of q over a 4-bit cache, with with_lse also float32 [B, Mq, H_q] log-sum-exps.
+    lens int32 [B]: keys of each sequence (n if None); row_map int32 [B, n]: cache row of each (b * n + j if None; an entry
+    that is no row: no such key)."""
+    code, tdt = _DTYPES[dtype]
+    B, Mq = q.shape[0], q.shape[1]
+    qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
+    kp, vp = (_need_cache(name, "kv4", t, cache_rows, H_kv, d_h) for name, t in (("k_cache", k_cache), ("v_cache", v_cache)))
+    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
+    out = torch.empty_like(q)
+    lse = torch.empty((B, Mq, H_q), dtype=torch.float32, device="cuda") if with_lse else None
+    nbytes = lib().dllmc_op_attention_kv4_scratch_bytes(code, B, Mq, n, H_q, H_kv, d_h)
+    scratch = _scratch(nbytes)
+    _check(lib().dllmc_op_attention_kv4(code, qp, B, Mq, kp, vp, cache_rows, rp, lp, n, H_q, H_kv, d_h, out.data_ptr(),
+                                        _ptr(lse), _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_kv4")
+    return (out, lse) if with_lse else out
+
+
+def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache: torch.Tensor, cache_rows: int, n: int,
+                         H_q: int, H_kv: int, d_h: int, lens: Optional[torch.Tensor] = None,
+                         row_map: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         acc: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """float32 [B, n]: acc (0 if None) plus the attention weight that q gives to every cached position.  cache_format: the
+    dtype, or "kv4".  lse: of op_attention_kv4 over the same operands, if there is one.  out: where it goes (may be acc)."""
+    code, tdt = _DTYPES[dtype]
+    fmt = _format(cache_format)
+    B, Mq = q.shape[0], q.shape[1]
+    qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
+    kp = _need_cache("k_cache", cache_format, k_cache, cache_rows, H_kv, d_h)
+    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
+    sp, ap = _need("lse", lse, torch.float32, (B, Mq, H_q)), _need("acc", acc, torch.float32, (B, n))
+    if out is None:
+        out = torch.empty((B, n), dtype=torch.float32, device="cuda")
+    op = _need("out", out, torch.float32, (B, n))
+    nbytes = lib().dllmc_op_attention_weights_scratch_bytes(code, fmt, B, Mq, n, H_q, H_kv, d_h)
+    scratch = _scratch(nbytes)
+    _check(lib().dllmc_op_attention_weights(code, fmt, qp, B, Mq, kp, cache_rows, rp, lp, n, H_q, H_kv, d_h, sp, ap, op,
+                                            _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_weights")
+    return out
+
+
+def op_evict(acc: torch.Tensor, keep: int, cache_rows: int, first: int = 0, last: int = 0,
+             lens: Optional[torch.Tensor] = None, row_map: Optional[torch.Tensor] = None):
+    """(kept [B, keep], kept_rows [B, keep], new_lens [B] int32, acc [B, keep] float32): the positions that stay, see
+    dllmc_op_evict."""
+    B, n = acc.shape
+    ap = _need("acc", acc, torch.float32, (B, n))
+    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
+    kept, kept_rows = (torch.empty((B, max(keep, 0)), dtype=torch.int32, device="cuda") for _ in range(2))
+    new_lens = torch.empty(B, dtype=torch.int32, device="cuda")
+    left = torch.empty((B, max(keep, 0)), dtype=torch.float32, device="cuda")
+    _check(lib().dllmc_op_evict(ap, B, n, lp, rp, cache_rows, keep, first, last, kept.data_ptr(), kept_rows.data_ptr(),
+                                new_lens.data_ptr(), left.data_ptr(), _stream_handle()), "dllmc_op_evict")
+    return kept, kept_rows, new_lens, left
+
+
+def op_compact(cache_format: str, rows: torch.Tensor, src_rows: int, H: int, d_h: int, k_src: torch.Tensor,
+               k_dst: torch.Tensor, v_src: Optional[torch.Tensor] = None, v_dst: Optional[torch.Tensor] = None,
+               dst_rows: Optional[int] = None) -> None:
+    """Row i of the destinations (dst_rows rows, as many as `rows` has if None) = row rows[i] of the sources; an entry that
+    is no row leaves row i as it was.  rows: int32 of any shape, taken flat.  Formats: "f32", "bf16", "kv4"."""
+    M = rows.numel()
+    dst_rows = M if dst_rows is None else dst_rows
+    rp = _need("rows", rows, torch.int32, rows.shape)
+    tensors = [None if t is None else _need_cache(name, cache_format, t, r, H, d_h)
+               for name, t, r in (("k_src", k_src, src_rows), ("k_dst", k_dst, dst_rows), ("v_src", v_src, src_rows),
+                                  ("v_dst", v_dst, dst_rows))]
+    _check(lib().dllmc_op_compact(_format(cache_format), rp, M, src_rows, dst_rows, H, d_h, *tensors, _stream_handle()),
+           "dllmc_op_compact")
+
+
+def i8_row_bytes(K: int) -> int:
+    """Bytes of a row of K 8-bit integers: K rounded up to 128."""
+    n = lib().dllmc_i8_row_bytes(K)
+    if n == 0:
+        raise DllmcError(f"dllmc_i8_row_bytes: no 8-bit rows of {K}")
+    return n
+
+
+def op_quant8(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = None):
+    """(int8 [M, i8_row_bytes(K)], float32 [M]): rows of x [*, K] (those that row_idx int32 [M] names) and their scales."""
+    code, tdt = _DTYPES[dtype]
+    K = x.shape[1]
+    M = x.shape[0] if row_idx is None else row_idx.numel()
+    xp, rp = _need("x", x, tdt, x.shape), _need("row_idx", row_idx, torch.int32, (M,))
+    q = torch.empty((M, i8_row_bytes(K)), dtype=torch.int8, device="cuda")
+    scale = torch.empty(M, dtype=torch.float32, device="cuda")
+    _check(lib().dllmc_op_quant8(code, xp, rp, M, K, q.data_ptr(), scale.data_ptr(), _stream_handle()), "dllmc_op_quant8")
+    return q, scale
+
+
+def op_linear_i8(dtype: str, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                 K: int) -> torch.Tensor:
+    """[M, N] of dtype: rows a times rows w (both as op_quant8 gives them, K integers each), scales multiplied in."""
+    code, tdt = _DTYPES[dtype]
+    M, N, kp = a.shape[0], w.shape[0], i8_row_bytes(K)
+    ap, wp = _need("a", a, torch.int8, (M, kp)), _need("w", w, torch.int8, (N, kp))
+    sa, sw = _need("a_scale", a_scale, torch.float32, (M,)), _need("w_scale", w_scale, torch.float32, (N,))
+    out = torch.empty((M, N), dtype=tdt, device="cuda")
+    nbytes = lib().dllmc_op_linear_i8_scratch_bytes(M, N, K)
+    scratch = _scratch(nbytes)
+    _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream_handle()),
+           "dllmc_op_linear_i8")
     return out
 
 

@@ -9,6 +9,7 @@
 
 #include "../../include/dllmc.h"
 #include "common.hpp"
+#include "kv4.hpp"
 #include "paging_host.hpp"
 
 using namespace dllmc;
@@ -1145,6 +1146,236 @@ int dllmc_probe_mfma(int32_t iters, int32_t shape, float* sink, double* flops_ou
   (void)hipGetLastError();
   const double f = launch_probe_mfma(iters, shape, sink, static_cast<hipStream_t>(hip_stream));
   if (flops_out) *flops_out = f;
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+}  // extern "C"
+
+// ---- the step's pieces in fewer bits ------------------------------------------------------------
+
+namespace {
+inline bool dtype_ok(int32_t t) { return t == DLLMC_F32 || t == DLLMC_BF16; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline size_t elem_bytes(int32_t dtype) { return dtype == DLLMC_BF16 ? 2 : 4; }
+
+constexpr int kMaxRows = 1 << 24;  // rows of a cache, positions of a batch (as for a context)
+constexpr int kMaxWidth = 1 << 16;  // H * d_h
+constexpr int kMaxI8K = 1 << 17;   // 127 * 127 * 2^17 < 2^31: a whole contraction fits an int32 sum
+
+bool kv4_shape_ok(int32_t rows, int32_t H, int32_t d_h) {
+  return rows >= 1 && rows <= kMaxRows && H >= 1 && d_h >= 32 && d_h % 32 == 0 && H <= kMaxWidth / d_h;
+}
+
+// heads, lengths and the cache of the operations that attend
+bool attend_shape_ok(int32_t B, int32_t Mq, int32_t cache_rows, const int32_t* row_map, const int32_t* lens, int32_t n, int32_t H_q,
+                     int32_t H_kv, int32_t d_h) {
+  if (B < 1 || Mq < 1 || n < 1 || H_kv < 1 || H_q < H_kv || H_q % H_kv || (d_h != 64 && d_h != 128 && d_h != 256)) return false;
+  if (cache_rows < 1 || cache_rows > kMaxRows || n > kMaxRows / B || H_q > kMaxWidth / d_h || Mq > kMaxRows / B) return false;
+  if (static_cast<long long>(B) * Mq * H_q > (1ll << 30)) return false;
+  if (row_map == nullptr && static_cast<long long>(B) * n > cache_rows) return false;
+  return aligned4(row_map) && aligned4(lens);
+}
+
+size_t cache_bytes(int32_t format, int32_t rows, int32_t H, int32_t d_h) {
+  return format == DLLMC_KV4 ? kv4_bytes(rows, H, d_h) : static_cast<size_t>(rows) * H * d_h * elem_bytes(format);
+}
+
+CacheView cache_view(int32_t format, const void* p, int32_t rows, int32_t H, int32_t d_h) {
+  CacheView c{p, Kv4Tensor{nullptr, nullptr}, rows, H};
+  if (format == DLLMC_KV4) c.kv4 = kv4_tensor(p, rows, H, d_h);
+  return c;
+}
+}  // namespace
+
+extern "C" {
+
+size_t dllmc_kv4_bytes(int32_t cache_rows, int32_t H, int32_t d_h) {
+  return kv4_shape_ok(cache_rows, H, d_h) ? kv4_bytes(cache_rows, H, d_h) : 0;
+}
+
+int dllmc_op_kv4_store(int32_t dtype, const void* x, int32_t M, const int32_t* rows, void* cache, int32_t cache_rows, int32_t H,
+                       int32_t d_h, void* hip_stream) {
+  if (!dtype_ok(dtype) || !x || !cache || M < 1 || M > kMaxRows || !kv4_shape_ok(cache_rows, H, d_h) || !aligned16(x) ||
+      !aligned16(cache) || !aligned4(rows) || (rows == nullptr && M > cache_rows))
+    return DLLMC_EINVAL;
+  const size_t cb = kv4_bytes(cache_rows, H, d_h);
+  if (!apart(cache, cb, x, static_cast<size_t>(M) * H * d_h * elem_bytes(dtype)) ||
+      (rows && !apart(cache, cb, rows, static_cast<size_t>(M) * 4)))
+    return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_kv4_store(dtype, x, M, H * d_h, rows, kv4_tensor(cache, cache_rows, H, d_h), cache_rows, d_h,
+                   static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int32_t H, int32_t d_h, const int32_t* rows, int32_t M,
+                      void* out, void* hip_stream) {
+  if (!dtype_ok(dtype) || !out || !cache || M < 1 || M > kMaxRows || !kv4_shape_ok(cache_rows, H, d_h) || !aligned16(out) ||
+      !aligned16(cache) || !aligned4(rows) || (rows == nullptr && M > cache_rows))
+    return DLLMC_EINVAL;
+  const size_t ob = static_cast<size_t>(M) * H * d_h * elem_bytes(dtype);
+  if (!apart(out, ob, cache, kv4_bytes(cache_rows, H, d_h)) || (rows && !apart(out, ob, rows, static_cast<size_t>(M) * 4)))
+    return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_kv4_load(dtype, kv4_tensor(cache, cache_rows, H, d_h), cache_rows, d_h, rows, M, H * d_h, out,
+                  static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_op_attention_kv4_scratch_bytes(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv,
+                                            int32_t d_h) {
+  static const int32_t some = 0;
+  if (!dtype_ok(dtype) || !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h)) return 0;
+  return attention_kv4_scratch_bytes(dtype, B, Mq, n, H_q, H_kv, d_h);
+}
+
+int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, const void* k_cache, const void* v_cache,
+                           int32_t cache_rows, const int32_t* row_map, const int32_t* lens, int32_t n, int32_t H_q, int32_t H_kv,
+                           int32_t d_h, void* out, float* lse, void* scratch, size_t scratch_bytes, void* hip_stream) {
+  if (!dtype_ok(dtype) || !q || !k_cache || !v_cache || !out ||
+      !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !aligned16(q) || !aligned16(k_cache) ||
+      !aligned16(v_cache) || !aligned16(out) || !aligned4(lse) || !aligned16(scratch))
+    return DLLMC_EINVAL;
+  const size_t need = attention_kv4_scratch_bytes(dtype, B, Mq, n, H_q, H_kv, d_h);
+  const size_t rows = static_cast<size_t>(B) * Mq * H_q, qb = rows * d_h * elem_bytes(dtype), cb = kv4_bytes(cache_rows, H_kv, d_h);
+  const struct { const void* p; size_t n; } in[] = {{q, qb}, {k_cache, cb}, {v_cache, cb},
+                                                    {row_map, row_map ? static_cast<size_t>(B) * n * 4 : 0}, {lens, lens ? static_cast<size_t>(B) * 4 : 0}};
+  if (lse && !apart(lse, rows * 4, out, qb)) return DLLMC_EINVAL;
+  for (const auto& i : in)
+    if (i.n && (!apart(out, qb, i.p, i.n) || (lse && !apart(lse, rows * 4, i.p, i.n)))) return DLLMC_EINVAL;
+  if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  (void)hipGetLastError();
+  launch_attention_kv4(dtype, q, B, Mq, cache_view(DLLMC_KV4, k_cache, cache_rows, H_kv, d_h),
+                       cache_view(DLLMC_KV4, v_cache, cache_rows, H_kv, d_h), Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, out,
+                       lse, scratch, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n, int32_t H_q,
+                                                int32_t H_kv, int32_t d_h) {
+  static const int32_t some = 0;
+  if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) ||
+      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h))
+    return 0;
+  return attention_weights_scratch_bytes(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+}
+
+int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* q, int32_t B, int32_t Mq, const void* k_cache,
+                               int32_t cache_rows, const int32_t* row_map, const int32_t* lens, int32_t n, int32_t H_q, int32_t H_kv,
+                               int32_t d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
+                               size_t scratch_bytes, void* hip_stream) {
+  if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) || !q || !k_cache || !acc_out ||
+      !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !aligned16(q) || !aligned16(k_cache) ||
+      !aligned4(lse) || !aligned4(acc_in) || !aligned4(acc_out) || !aligned16(scratch))
+    return DLLMC_EINVAL;
+  const size_t need = attention_weights_scratch_bytes(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+  const size_t rows = static_cast<size_t>(B) * Mq * H_q, ob = static_cast<size_t>(B) * n * 4;
+  const struct { const void* p; size_t n; } in[] = {{q, rows * d_h * elem_bytes(dtype)}, {k_cache, cache_bytes(cache_format, cache_rows, H_kv, d_h)},
+                                                    {row_map, row_map ? ob : 0}, {lens, lens ? static_cast<size_t>(B) * 4 : 0},
+                                                    {lse, lse ? rows * 4 : 0}, {acc_in, acc_in && acc_in != acc_out ? ob : 0}};
+  for (const auto& i : in)
+    if (i.n && !apart(acc_out, ob, i.p, i.n)) return DLLMC_EINVAL;
+  if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  (void)hipGetLastError();
+  launch_attention_weights(dtype, cache_format, q, B, Mq, cache_view(cache_format, k_cache, cache_rows, H_kv, d_h),
+                           Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, lse, acc_in, acc_out, scratch,
+                           static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_evict(const float* acc, int32_t B, int32_t n, const int32_t* lens, const int32_t* row_map, int32_t cache_rows,
+                   int32_t keep, int32_t first, int32_t last, int32_t* kept, int32_t* kept_rows, int32_t* new_lens, float* acc_out,
+                   void* hip_stream) {
+  if (!acc || !kept || !kept_rows || !new_lens || B < 1 || n < 1 || n > kMaxRows / B || cache_rows < 1 || cache_rows > kMaxRows ||
+      keep < 1 || keep > n || first < 0 || last < 0 || first > keep || last > keep - first || !aligned4(acc) || !aligned4(lens) ||
+      !aligned4(row_map) || !aligned4(kept) || !aligned4(kept_rows) || !aligned4(new_lens) || !aligned4(acc_out) ||
+      (row_map == nullptr && static_cast<long long>(B) * n > cache_rows))
+    return DLLMC_EINVAL;
+  const size_t bn = static_cast<size_t>(B) * n * 4, bk = static_cast<size_t>(B) * keep * 4, b4 = static_cast<size_t>(B) * 4;
+  const struct { const void* p; size_t n; } in[] = {{acc, bn}, {row_map, row_map ? bn : 0}, {lens, lens ? b4 : 0}},
+                                            to[] = {{kept, bk}, {kept_rows, bk}, {new_lens, b4}, {acc_out, acc_out ? bk : 0}};
+  for (int t = 0; t < 4; ++t) {
+    if (!to[t].n) continue;
+    for (const auto& i : in)
+      if (i.n && !apart(to[t].p, to[t].n, i.p, i.n)) return DLLMC_EINVAL;
+    for (int u = t + 1; u < 4; ++u)
+      if (to[u].n && !apart(to[t].p, to[t].n, to[u].p, to[u].n)) return DLLMC_EINVAL;
+  }
+  (void)hipGetLastError();
+  launch_evict(acc, B, Keys{lens, row_map, n, cache_rows}, keep, first, last, kept, kept_rows, new_lens, acc_out,
+               static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32_t src_rows, int32_t dst_rows, int32_t H, int32_t d_h,
+                     const void* k_src, void* k_dst, const void* v_src, void* v_dst, void* hip_stream) {
+  const bool kv4 = cache_format == DLLMC_KV4;
+  if ((!kv4 && !dtype_ok(cache_format)) || !rows || !k_src || !k_dst || !v_src != !v_dst || M < 1 || src_rows < 1 ||
+      src_rows > kMaxRows || dst_rows < M || dst_rows > kMaxRows || H < 1 || d_h < 1 || H > kMaxWidth / d_h || !aligned4(rows))
+    return DLLMC_EINVAL;
+  const void* tensors[] = {k_src, k_dst, v_src, v_dst};
+  const uintptr_t piece = kv4 ? 16 : elem_bytes(cache_format);
+  if (kv4 && !kv4_shape_ok(src_rows, H, d_h)) return DLLMC_EINVAL;
+  for (const void* t : tensors)
+    if (reinterpret_cast<uintptr_t>(t) % piece) return DLLMC_EINVAL;
+  const size_t sb = cache_bytes(cache_format, src_rows, H, d_h), db = cache_bytes(cache_format, dst_rows, H, d_h);
+  for (int t = 1; t < 4; t += 2) {
+    if (!tensors[t]) continue;
+    if (!apart(tensors[t], db, k_src, sb) || (v_src && !apart(tensors[t], db, v_src, sb)) ||
+        !apart(tensors[t], db, rows, static_cast<size_t>(M) * 4))
+      return DLLMC_EINVAL;
+  }
+  if (v_dst && !apart(k_dst, db, v_dst, db)) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_compact(cache_format, rows, M, src_rows, dst_rows, H, d_h, k_src, k_dst, v_src, v_dst, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_i8_row_bytes(int32_t K) { return K >= 1 && K <= kMaxI8K ? i8_row_bytes(K) : 0; }
+
+int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
+                    void* hip_stream) {
+  if (!dtype_ok(dtype) || !x || !q || !scale || M < 1 || M > kMaxRows || K < 1 || K > kMaxI8K || !aligned16(q) || !aligned4(scale) ||
+      !aligned4(row_idx) || reinterpret_cast<uintptr_t>(x) % elem_bytes(dtype))
+    return DLLMC_EINVAL;
+  const size_t qb = M * i8_row_bytes(K), sb = static_cast<size_t>(M) * 4;
+  // (a gathered x has more rows than the call says: it has to lie clear of both results in the rows it names, which is the caller's to see to)
+  const size_t xb = (row_idx ? 1 : static_cast<size_t>(M)) * K * elem_bytes(dtype);
+  if (!apart(q, qb, x, xb) || !apart(scale, sb, x, xb) || !apart(q, qb, scale, sb) ||
+      (row_idx && (!apart(q, qb, row_idx, sb) || !apart(scale, sb, row_idx, sb))))
+    return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_quant8(dtype, x, row_idx, M, K, q, scale, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K) {
+  if (M < 1 || M > kMaxRows || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return 0;
+  return linear_i8_scratch_bytes(M, N, K);
+}
+
+int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int32_t M, const int8_t* w, const float* w_scale,
+                       int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes, void* hip_stream) {
+  if (!dtype_ok(dtype) || !a || !a_scale || !w || !w_scale || !out || M < 1 || M > kMaxRows || N < 1 || N > kMaxRows || K < 1 ||
+      K > kMaxI8K || !aligned16(a) || !aligned16(w) || !aligned4(a_scale) || !aligned4(w_scale) ||
+      reinterpret_cast<uintptr_t>(out) % elem_bytes(dtype) || !aligned16(scratch))
+    return DLLMC_EINVAL;
+  const size_t need = linear_i8_scratch_bytes(M, N, K), kp = i8_row_bytes(K);
+  const size_t ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
+  if (!apart(out, ob, a, M * kp) || !apart(out, ob, w, N * kp) || !apart(out, ob, a_scale, static_cast<size_t>(M) * 4) ||
+      !apart(out, ob, w_scale, static_cast<size_t>(N) * 4))
+    return DLLMC_EINVAL;
+  if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  (void)hipGetLastError();
+  launch_linear_i8(dtype, a, a_scale, M, w, w_scale, N, K, out, scratch, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
   return DLLMC_OK;
 }

@@ -1,0 +1,222 @@
+// Eviction from a cache: the positions that stay under a budget, by accumulated attention weight, and their rows moved together.
+#include "kv4.hpp"
+
+namespace dllmc {
+
+namespace {
+
+constexpr int kEW = 16;  // wavefronts of the selection's workgroup
+
+// What positions are ordered by: 0 not there, then NaN, then the weights ascending (-0 as 0), then those always kept.
+__device__ __forceinline__ uint32_t keep_key(const float* acc, const Keys& keys, int b, int j, int len, int first, int last) {
+  if (j >= len || keys.row(b, j) < 0) return 0;
+  if (j < first || j >= len - last) return 0xffffffffu;
+  const float w = acc[static_cast<size_t>(b) * keys.n + j] + 0.f;
+  if (w != w) return 1;
+  const uint32_t u = __float_as_uint(w);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// One workgroup per sequence.  Wavefront w takes the positions [w P, (w + 1) P), P = 64 KPT, 64 neighbours at a time, so that
+// the order of positions is the order of (wavefront, trip, lane) and places come from ballots.  The k-th largest key by four
+// passes over its bytes; each pass counts the keys that agree with the bytes found so far in a histogram with a column per
+// lane (weights of one sequence share their exponents: in a single column most of a wavefront's adds would meet).
+// KPT > 0: keys in registers; 0: formed again in every pass.
+template <int KPT>
+__global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ acc, Keys keys, int keep, int first, int last,
+                                                    int* __restrict__ kept, int* __restrict__ kept_rows,
+                                                    int* __restrict__ new_lens, float* __restrict__ acc_out) {
+  __shared__ uint32_t hist[256 * 64];
+  __shared__ int bins[256], found[3], counts[2][kEW];
+  const int b = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int trips = KPT > 0 ? KPT : (keys.n + 64 * kEW - 1) / (64 * kEW);
+  const int len = keys.length(b), j0 = wave * trips * 64 + lane;
+  uint32_t held[KPT > 0 ? KPT : 1];
+  auto key = [&](int i) -> uint32_t {
+    if constexpr (KPT > 0) return held[i];
+    return keep_key(acc, keys, b, j0 + i * 64, len, first, last);
+  };
+  auto each = [&](auto&& f) {
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) f(i);
+    } else {
+      for (int i = 0; i < trips; ++i) f(i);
+    }
+  };
+  if constexpr (KPT > 0) {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) held[i] = keep_key(acc, keys, b, j0 + i * 64, len, first, last);
+  }
+  int mine = 0;
+  each([&](int i) { mine += __popcll(__ballot(key(i) != 0)); });
+  if (lane == 0) counts[0][wave] = mine;
+  __syncthreads();
+  int there = 0;
+  for (int w = 0; w < kEW; ++w) there += counts[0][w];
+  const int k = min(keep, there);
+
+  // threshold: keys above it all stay, `quota` of those equal to it, the lowest positions
+  uint32_t threshold = 0;
+  int quota = 0;
+  if (there > keep) {
+    int want = k;  // of the keys that agree with the bytes found so far
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int t = threadIdx.x; t < 256 * 64; t += 64 * kEW) hist[t] = 0;
+      __syncthreads();
+      each([&](int i) {
+        const uint32_t u = key(i);
+        if (u != 0 && (shift == 24 || (u >> (shift + 8)) == (threshold >> (shift + 8)))) atomicAdd(&hist[((u >> shift) & 255) * 64 + lane], 1u);
+      });
+      __syncthreads();
+      {
+        const int bin = threadIdx.x / 4, part = threadIdx.x % 4;
+        int sum = 0;
+        for (int t = 0; t < 16; ++t) sum += hist[bin * 64 + part * 16 + (t + threadIdx.x) % 16];
+        sum += __shfl_xor(sum, 1, 64);
+        sum += __shfl_xor(sum, 2, 64);
+        if (part == 0) bins[bin] = sum;
+      }
+      __syncthreads();
+      if (wave == 0) {
+        int c[4], above = 0;
+        for (int t = 0; t < 4; ++t) above += c[t] = bins[lane * 4 + t];
+        const int own = above;
+        for (int o = 1; o < 64; o <<= 1) {
+          const int v = __shfl_down(above, o, 64);
+          if (lane + o < 64) above += v;
+        }
+        above -= own;  // keys in the bins of the lanes after this one
+        for (int t = 3; t >= 0; --t) {
+          if (above < want && above + c[t] >= want) {
+            found[0] = lane * 4 + t;
+            found[1] = above;
+          }
+          above += c[t];
+        }
+      }
+      __syncthreads();
+      threshold |= static_cast<uint32_t>(found[0]) << shift;
+      want -= found[1];
+      __syncthreads();
+    }
+    quota = want;
+  }
+  // places: of a position that stays, the number of those before it
+  int above = 0, equal = 0;
+  each([&](int i) {
+    const uint32_t u = key(i);
+    above += __popcll(__ballot(u > threshold));
+    equal += __popcll(__ballot(u == threshold && u != 0));
+  });
+  __syncthreads();
+  if (lane == 0) {
+    counts[0][wave] = above;
+    counts[1][wave] = equal;
+  }
+  __syncthreads();
+  above = equal = 0;
+  for (int w = 0; w < wave; ++w) {
+    above += counts[0][w];
+    equal += counts[1][w];
+  }
+  const size_t out0 = static_cast<size_t>(b) * keep;
+  each([&](int i) {
+    const uint32_t u = key(i);
+    const uint64_t hi = __ballot(u > threshold), eq = __ballot(u == threshold && u != 0);
+    const uint64_t below = (1ull << lane) - 1;
+    const int hb = above + __popcll(hi & below), eb = equal + __popcll(eq & below);
+    if (u > threshold || (u == threshold && u != 0 && eb < quota)) {
+      const size_t at = out0 + hb + min(eb, quota);
+      const int j = j0 + i * 64;
+      kept[at] = j;
+      kept_rows[at] = keys.row(b, j);
+      if (acc_out != nullptr) acc_out[at] = acc[static_cast<size_t>(b) * keys.n + j];
+    }
+    above += __popcll(hi);
+    equal += __popcll(eq);
+  });
+  for (int t = k + threadIdx.x; t < keep; t += 64 * kEW) {
+    kept[out0 + t] = -1;
+    kept_rows[out0 + t] = -1;
+    if (acc_out != nullptr) acc_out[out0 + t] = 0.f;
+  }
+  if (threadIdx.x == 0) new_lens[b] = k;
+}
+
+// dst row i = src row rows[i]: rows of `pieces` units
+template <typename U>
+__global__ __launch_bounds__(256) void k_compact_rows(const int* __restrict__ rows, int M, int src_rows, long long pieces,
+                                                      const U* __restrict__ k_src, U* __restrict__ k_dst,
+                                                      const U* __restrict__ v_src, U* __restrict__ v_dst) {
+  const long long all = M * pieces;
+  for (long long p = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; p < all; p += static_cast<long long>(gridDim.x) * 256) {
+    const int row = rows[p / pieces];
+    if (static_cast<unsigned>(row) >= static_cast<unsigned>(src_rows)) continue;
+    const size_t from = static_cast<size_t>(row) * pieces + p % pieces;
+    const U k = k_src[from];
+    if (v_src != nullptr) v_dst[p] = v_src[from];
+    k_dst[p] = k;
+  }
+}
+
+// the same for 4-bit tensors: a piece is 32 elements, 16 bytes of codes and a scale
+__global__ __launch_bounds__(256) void k_compact_kv4(const int* __restrict__ rows, int M, int src_rows, int dst_rows, int H,
+                                                     int blocks, Kv4Tensor ks, Kv4Tensor kd, Kv4Tensor vs, Kv4Tensor vd) {
+  const long long all = static_cast<long long>(M) * H * blocks;
+  for (long long p = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; p < all; p += static_cast<long long>(gridDim.x) * 256) {
+    const int g = static_cast<int>(p % blocks), i = static_cast<int>(p / blocks % M), h = static_cast<int>(p / blocks / M);
+    const int row = rows[i];
+    if (static_cast<unsigned>(row) >= static_cast<unsigned>(src_rows)) continue;
+    const size_t from = (static_cast<size_t>(h) * src_rows + row) * blocks + g, to = (static_cast<size_t>(h) * dst_rows + i) * blocks + g;
+    reinterpret_cast<uint4*>(kd.codes)[to] = reinterpret_cast<const uint4*>(ks.codes)[from];
+    kd.scales[to] = ks.scales[from];
+    if (vs.codes != nullptr) {
+      reinterpret_cast<uint4*>(vd.codes)[to] = reinterpret_cast<const uint4*>(vs.codes)[from];
+      vd.scales[to] = vs.scales[from];
+    }
+  }
+}
+
+inline unsigned groups(long long items) {
+  const long long g = (items + 255) / 256;
+  return static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20);
+}
+
+}  // namespace
+
+void launch_evict(const float* acc, int B, const Keys& keys, int keep, int first, int last, int* kept, int* kept_rows,
+                  int* new_lens, float* acc_out, hipStream_t st) {
+#define DLLMC_E(KPT) \
+  hipLaunchKernelGGL(k_evict<KPT>, dim3(B), dim3(64 * kEW), 0, st, acc, keys, keep, first, last, kept, kept_rows, new_lens, acc_out)
+  const int n = keys.n;
+  if (n <= 1024) DLLMC_E(1);
+  else if (n <= 4096) DLLMC_E(4);
+  else if (n <= 16384) DLLMC_E(16);
+  else DLLMC_E(0);
+#undef DLLMC_E
+}
+
+void launch_compact(int format, const int* rows, int M, int src_rows, int dst_rows, int H, int d_h, const void* k_src, void* k_dst,
+                    const void* v_src, void* v_dst, hipStream_t st) {
+  if (format == 2) {
+    const Kv4Tensor none{nullptr, nullptr};
+    hipLaunchKernelGGL(k_compact_kv4, dim3(groups(static_cast<long long>(M) * H * (d_h / 32))), dim3(256), 0, st, rows, M, src_rows,
+                       dst_rows, H, d_h / 32, kv4_tensor(k_src, src_rows, H, d_h), kv4_tensor(k_dst, dst_rows, H, d_h),
+                       v_src ? kv4_tensor(v_src, src_rows, H, d_h) : none, v_src ? kv4_tensor(v_dst, dst_rows, H, d_h) : none);
+    return;
+  }
+  const size_t bytes = static_cast<size_t>(H) * d_h * (format == 1 ? 2 : 4);
+  const uintptr_t any = reinterpret_cast<uintptr_t>(k_src) | reinterpret_cast<uintptr_t>(k_dst) | reinterpret_cast<uintptr_t>(v_src) |
+                        reinterpret_cast<uintptr_t>(v_dst) | bytes;
+  auto go = [&](auto u) {
+    typedef decltype(u) U;
+    const long long pieces = static_cast<long long>(bytes / sizeof(U));
+    hipLaunchKernelGGL(k_compact_rows<U>, dim3(groups(M * pieces)), dim3(256), 0, st, rows, M, src_rows, pieces,
+                       static_cast<const U*>(k_src), static_cast<U*>(k_dst), static_cast<const U*>(v_src), static_cast<U*>(v_dst));
+  };
+  if (any % 16 == 0) go(uint4());
+  else go(uint16_t());
+}
+
+}  // namespace dllmc

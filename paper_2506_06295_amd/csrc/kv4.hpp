@@ -1,0 +1,101 @@
+// 4-bit cache tensors as kernels see them, and which cached keys of a sequence there are.
+#pragma once
+
+#include "common.hpp"
+
+namespace dllmc {
+
+// codes [H][rows][d_h / 2], scales [H][rows][d_h / 32]
+struct Kv4Tensor {
+  uint8_t* codes;
+  uint8_t* scales;
+};
+inline size_t kv4_code_bytes(int cache_rows, int H, int d_h) {
+  return (static_cast<size_t>(cache_rows) * H * (d_h / 2) + 255) / 256 * 256;
+}
+inline size_t kv4_bytes(int cache_rows, int H, int d_h) {
+  return kv4_code_bytes(cache_rows, H, d_h) + static_cast<size_t>(cache_rows) * H * (d_h / 32);
+}
+inline Kv4Tensor kv4_tensor(const void* p, int cache_rows, int H, int d_h) {
+  uint8_t* codes = static_cast<uint8_t*>(const_cast<void*>(p));
+  return Kv4Tensor{codes, codes + kv4_code_bytes(cache_rows, H, d_h)};
+}
+
+// A cache tensor of one of the formats: `rows` is [cache_rows][H][d_h] of the model dtype, or `kv4`.
+struct CacheView {
+  const void* rows;
+  Kv4Tensor kv4;
+  int cache_rows, H;
+};
+
+// Which keys a sequence has: position j < min(lens[b], n) whose cache row, row_map[b * n + j] or b * n + j, lies in the cache.
+struct Keys {
+  const int* lens;
+  const int* row_map;
+  int n, cache_rows;
+  __device__ __forceinline__ int length(int b) const { return lens ? max(0, min(lens[b], n)) : n; }
+  // cache row of position j < n, negative if it is not there
+  __device__ __forceinline__ int row(int b, int j) const {
+    const int r = row_map ? row_map[static_cast<size_t>(b) * n + j] : b * n + j;
+    return static_cast<unsigned>(r) < static_cast<unsigned>(cache_rows) ? r : -1;
+  }
+};
+
+// Scale byte of a block whose largest magnitude has the bits `top`: 127 + the smallest e with top <= 6 * 2^e = 1.5 * 2^(e + 2), so
+// that nothing saturates; at least 2 (no value below 2^-126), at most 252 (6 * 2^125 is finite: above it values do saturate).
+__device__ __forceinline__ uint32_t kv4_scale_byte(uint32_t top) {
+  if (top >= 0x7f800000u) return 255;
+  const int e = static_cast<int>(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
+  return static_cast<uint32_t>(max(2, min(252, e)));
+}
+
+// eight codes times 2^(scale - 127), exact; NaN for scale 255 (the conversion takes the exponent bits of its scale)
+__device__ __forceinline__ bf16x8 kv4_expand(uint32_t w, uint32_t scale) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const float s = __uint_as_float(scale << 23);
+  const uint4 r = make_uint4(__builtin_bit_cast(uint32_t, bf16x2_t(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0))),
+                             __builtin_bit_cast(uint32_t, bf16x2_t(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1))),
+                             __builtin_bit_cast(uint32_t, bf16x2_t(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2))),
+                             __builtin_bit_cast(uint32_t, bf16x2_t(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))));
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// element t of a cached row's head h
+template <typename C> __device__ __forceinline__ float cache_at(const CacheView& c, int h, int row, int t, int d_h) {
+  return ldf(static_cast<const C*>(c.rows) + (static_cast<size_t>(row) * c.H + h) * d_h + t);
+}
+template <> __device__ __forceinline__ float cache_at<Kv4Tensor>(const CacheView& c, int h, int row, int t, int d_h) {
+  const size_t at = static_cast<size_t>(h) * c.cache_rows + row;
+  const uint32_t byte = c.kv4.codes[at * (d_h / 2) + t / 2], scale = c.kv4.scales[at * (d_h / 32) + t / 32];
+  const uint4 v = __builtin_bit_cast(uint4, kv4_expand(byte, scale));
+  return __uint_as_float(t % 2 ? v.x & 0xffff0000u : v.x << 16);
+}
+
+void launch_kv4_store(int dtype, const void* x, int M, int width, const int* rows, Kv4Tensor c, int cache_rows, int d_h,
+                      hipStream_t st);
+void launch_kv4_load(int dtype, Kv4Tensor c, int cache_rows, int d_h, const int* rows, int M, int width, void* out,
+                     hipStream_t st);
+
+// Attention over a 4-bit cache, and the weights that cached positions get; scratch as large as the functions say.
+size_t attention_kv4_scratch_bytes(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h);
+void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
+                          int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st);
+size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h);
+void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
+                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
+                              hipStream_t st);
+
+// Which positions stay (kernels_evict.hip), and rows moved: dst row i = src row rows[i] for i < M where that is one.
+void launch_evict(const float* acc, int B, const Keys& keys, int keep, int first, int last, int* kept, int* kept_rows,
+                  int* new_lens, float* acc_out, hipStream_t st);
+void launch_compact(int format, const int* rows, int M, int src_rows, int dst_rows, int H, int d_h, const void* k_src, void* k_dst,
+                    const void* v_src, void* v_dst, hipStream_t st);
+
+// 8-bit rows of K rounded up to 128 bytes (kernels_i8.hip)
+inline size_t i8_row_bytes(int K) { return (static_cast<size_t>(K) + 127) / 128 * 128; }
+void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st);
+size_t linear_i8_scratch_bytes(int M, int N, int K);
+void launch_linear_i8(int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale, int N, int K,
+                      void* out, void* scratch, hipStream_t st);
+
+}  // namespace dllmc

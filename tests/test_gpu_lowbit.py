@@ -1,0 +1,386 @@
+"""GPU tests of the operators in fewer bits against plain 64-bit forms (tests/lowbit_ref.py).
+
+Tolerances are bounds, not experience: float32 sums and products of the sizes at hand, the exponentials' arguments, one rounding
+of the result to its type (half a step: 2^-24, 2^-8), and for bf16 attention probabilities as a bf16 pair (2^-16)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_06295_amd import binding as L
+from tests import lowbit_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+def host(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+# ------------------------------------------------------------------ 4-bit rows
+def special_rows(r, M, width, dtype):
+    x = r.standard_normal((M, width)) * np.exp(r.uniform(-20, 20, (M, width // 32)).repeat(32, 1))
+    x = R.grid(x, dtype).copy()
+    x[0, :32] = 0.0
+    if M > 1:
+        x[1, :16] = [0, -0.0, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, -.25, -.75, -1.25, -1.75, -2.5, -3.5, 6]   # every tie
+        x[1, 16:32] = 1.0
+        x[-1, 0] = np.inf
+        x[-1, 33 % width] = np.nan
+    if M > 2:
+        x[2, :32] = R.grid(np.full(32, 3.3e38), dtype)       # saturates: 6 * 2^125 is the largest value held
+        x[2, :4] = [1e38, -3e38, 2.0 ** 127, 6.0 * 2.0 ** 125]
+    if M > 3:
+        x[3, :32] = 2.0 ** -130                              # below the smallest scale's first level: zeros
+        x[3, 0:3] = [2.0 ** -127, 2.0 ** -126, -1.5 * 2.0 ** -125]
+    if M > 4:
+        x[4, :32] = 0.1
+        x[4, 5] = 6.0                                        # max = 6 * 2^0 exactly, then just above it
+        if width > 32:
+            x[4, 32:64] = 0.1
+            x[4, 40] = np.nextafter(np.float32(6), np.float32(7)) if dtype == "f32" else 6.03125
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,cache_rows,H,d_h", [(1, 1, 1, 32), (7, 20, 3, 64), (33, 40, 2, 128), (5, 9, 1, 256), (6, 64, 7, 96),
+                                               (130, 130, 4, 128)])
+def test_rows_in_and_out(dtype, M, cache_rows, H, d_h):
+    r = np.random.default_rng(M * 100 + d_h)
+    x = special_rows(r, M, H * d_h, dtype)
+    rows = r.permutation(cache_rows)[:M]
+    cache = torch.full((L.kv4_bytes(cache_rows, H, d_h),), 0x7b, dtype=torch.uint8, device="cuda")
+    before = L.op_kv4_load("f32", cache, cache_rows, H, d_h).cpu().numpy()
+    L.op_kv4_store(dtype, R.dev(x, dtype), cache, cache_rows, H, d_h, rows=R.ints(rows))
+    want = before.astype(np.float64)
+    want[rows] = R.kv4_values(x)
+    for out in ("f32", "bf16"):
+        got = host(L.op_kv4_load(out, cache, cache_rows, H, d_h))
+        assert np.array_equal(got, want, equal_nan=True)
+    pick = r.permutation(cache_rows)
+    assert np.array_equal(host(L.op_kv4_load("f32", cache, cache_rows, H, d_h, rows=R.ints(pick))), want[pick], equal_nan=True)
+
+
+def test_layout_is_the_documented_one():
+    r = np.random.default_rng(5)
+    rows, H, d_h = 11, 3, 64
+    x = R.grid(r.standard_normal((rows, H * d_h)), "bf16")
+    cache = torch.zeros(L.kv4_bytes(rows, H, d_h), dtype=torch.uint8, device="cuda")
+    L.op_kv4_store("bf16", R.dev(x, "bf16"), cache, rows, H, d_h)
+    assert np.array_equal(cache.cpu().numpy(), R.kv4_pack(x, H, d_h))
+
+
+def test_entries_that_are_no_row():
+    rows, H, d_h = 8, 2, 64
+    r = np.random.default_rng(6)
+    x = R.grid(r.standard_normal((5, H * d_h)), "f32")
+    cache = torch.zeros(L.kv4_bytes(rows, H, d_h), dtype=torch.uint8, device="cuda")
+    at = np.array([-1, 3, 8, 2 ** 31 - 1, 0])
+    L.op_kv4_store("f32", R.dev(x), cache, rows, H, d_h, rows=R.ints(at))
+    want = np.zeros((rows, H * d_h))
+    want[3], want[0] = R.kv4_values(x[1]), R.kv4_values(x[4])
+    assert np.array_equal(host(L.op_kv4_load("f32", cache, rows, H, d_h)), want)
+    got = host(L.op_kv4_load("f32", cache, rows, H, d_h, rows=R.ints([3, -5, 8, 0])))
+    assert np.array_equal(got, np.stack([want[3], 0 * want[3], 0 * want[3], want[0]]))
+
+
+# ------------------------------------------------------------------ attention and the weights of positions
+class Case:
+    """Queries and caches of a batch; cache rows that no key lies in are NaN in every format."""
+
+    def __init__(self, seed, dtype, B, Mq, n, H_q, H_kv, d_h, lens=None, mode="flat", q_scale=1.0):
+        r = self.r = np.random.default_rng(seed)
+        self.dtype, self.B, self.Mq, self.n, self.H_q, self.H_kv, self.d_h = dtype, B, Mq, n, H_q, H_kv, d_h
+        self.lens = lens
+        self.rows, self.row_map = B * n, None
+        if mode != "flat":
+            page = 5
+            pages = -(-n // page)
+            pool = B * pages + 2
+            table = r.permutation(pool)[:B * pages].reshape(B, pages)
+            self.row_map = (table[:, :, None] * page + np.arange(page)).reshape(B, -1)[:, :n].astype(np.int64)
+            self.rows = pool * page
+            if mode == "holes":
+                hole = r.random((B, n)) < 0.3
+                hole[0] = r.random() < 0.5      # a sequence that has nothing, or no hole at all
+                bad = r.choice([-1, -2 ** 31, self.rows, 2 ** 31 - 1], (B, n))
+                self.row_map = np.where(hole, bad, self.row_map)
+        self.where = R.present(B, n, self.rows, lens, self.row_map)
+        self.q = R.grid(q_scale * r.standard_normal((B, Mq, H_q, d_h)), dtype)
+        kv = [R.grid(r.standard_normal((self.rows, H_kv * d_h)) * np.exp(0.7 * r.standard_normal((1, H_kv * d_h))), dtype)
+              for _ in range(2)]
+        used = np.zeros(self.rows, bool)
+        for _, rows in self.where:
+            used[rows] = True
+        for x in kv:
+            x[~used] = np.nan
+        self.k, self.v = kv
+
+    def device(self, fmt):
+        def put(x):
+            if fmt != "kv4":
+                return R.dev(x, fmt)
+            c = torch.zeros(L.kv4_bytes(self.rows, self.H_kv, self.d_h), dtype=torch.uint8, device="cuda")
+            L.op_kv4_store("f32", R.dev(x), c, self.rows, self.H_kv, self.d_h)
+            return c
+        where = {"lens": None if self.lens is None else R.ints(self.lens),
+                 "row_map": None if self.row_map is None else R.ints(self.row_map)}
+        return R.dev(self.q.reshape(self.B, self.Mq, -1), self.dtype), put(self.k), put(self.v), where
+
+    def values(self, fmt, x):
+        x = np.where(np.isnan(x), 0, x)
+        x = R.kv4_values(x) if fmt == "kv4" else x.astype(np.float64)
+        return x.reshape(self.rows, self.H_kv, self.d_h)
+
+    def reference(self, fmt):
+        return R.attend(self.q.astype(np.float64), self.values(fmt, self.k), self.values(fmt, self.v), self.where, self.H_q,
+                        self.H_kv, self.d_h)
+
+
+def check_attention(c):
+    q, k, v, where = c.device("kv4")
+    out, lse = L.op_attention_kv4(c.dtype, q, k, v, c.rows, c.n, c.H_q, c.H_kv, c.d_h, with_lse=True, **where)
+    alone = L.op_attention_kv4(c.dtype, q, k, v, c.rows, c.n, c.H_q, c.H_kv, c.d_h, **where)
+    assert torch.equal(out, alone)
+    want, want_lse, _, mass, reach = c.reference("kv4")
+    got, got_lse = host(out).reshape(want.shape), lse.cpu().numpy().astype(np.float64)
+    ds = R.score_error(reach, want_lse, c.d_h)
+    tol_lse = ds + c.n * 2.0 ** -24 + np.abs(np.where(np.isfinite(want_lse), want_lse, 0)) * 2.0 ** -22
+    empty = ~np.isfinite(want_lse)
+    assert np.array_equal(np.isneginf(got_lse), empty)
+    assert (np.abs(got_lse[~empty] - want_lse[~empty]) <= tol_lse[~empty]).all()
+    # p_j moves by 2 ds relative; its rounding; sums of n terms and their quotient
+    rel = 2 * ds + c.n * 2.0 ** -23 + 2.0 ** -21 + (2.0 ** -16 if c.dtype == "bf16" else 0.0)
+    tol = mass * rel[..., None] + np.abs(want) * R.HALF_STEP[c.dtype] + 1e-40
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= tol).all(), np.max(np.abs(got - want) / tol)
+    assert (got[empty] == 0).all()
+
+
+def check_weights(c, fmt):
+    q, k, v, where = c.device(fmt)
+    acc = R.grid(c.r.random((c.B, c.n)), "f32")
+    args = (c.dtype, fmt, q, k, c.rows, c.n, c.H_q, c.H_kv, c.d_h)
+    got = L.op_attention_weights(*args, acc=R.dev(acc), **where)
+    bare = L.op_attention_weights(*args, **where)
+    _, lse, probs, _, reach = c.reference(fmt)
+    ds = R.score_error(reach, lse, c.d_h)
+    rows = c.Mq * c.H_q
+    # a probability below 2^-126, float32's smallest normal number, may come out as zero
+    want, tol = np.zeros((c.B, c.n)), np.full((c.B, c.n), rows * 2.0 ** -126)
+    for b, (pos, _) in enumerate(c.where):
+        for a in range(c.H_q):
+            p = probs[b][a]
+            want[b, pos] += p.sum(0)
+            # numerator and row sum each move by ds; sums of n and of Mq * H_q terms
+            tol[b, pos] += (p * (3 * ds[b, :, a] + (c.n + rows) * 2.0 ** -23 + 2.0 ** -20)[:, None]).sum(0)
+    assert (np.abs(host(bare) - want) <= tol).all()
+    assert (np.abs(host(got) - (want + acc)) <= tol + (want + acc) * 2.0 ** -23).all()
+    if fmt == "kv4":
+        # (a row sum that is rounded once more, as a logarithm of the size of a score: in ds)
+        _, lse_dev = L.op_attention_kv4(c.dtype, q, k, v, c.rows, c.n, c.H_q, c.H_kv, c.d_h, with_lse=True, **where)
+        given = L.op_attention_weights(*args, lse=lse_dev, **where)
+        assert (np.abs(host(given) - want) <= tol + want * 2.0 ** -21).all()
+    again = R.dev(acc)
+    assert L.op_attention_weights(*args, acc=again, out=again, **where) is again
+    assert torch.equal(again, got)
+
+
+SHAPES = [  # B, Mq, n, H_q, H_kv, d_h
+    (1, 1, 1, 1, 1, 64), (1, 1, 96, 4, 4, 64), (2, 3, 33, 4, 2, 64), (1, 17, 31, 2, 1, 128), (3, 5, 64, 7, 1, 128),
+    (1, 51, 200, 2, 2, 128), (2, 64, 65, 8, 2, 128), (1, 130, 129, 3, 3, 128), (2, 1, 700, 28, 4, 128), (1, 16, 257, 1, 1, 256),
+    (2, 40, 100, 4, 2, 256), (1, 300, 300, 2, 2, 64), (1, 129, 1030, 1, 1, 128), (1, 2, 5000, 2, 1, 128),
+]
+
+
+def lens_of(kind, B, n, r):
+    if kind == "all":
+        return None
+    if kind == "ragged":
+        return r.integers(1, n + 1, B)
+    some = np.array([0, 1, n, n + 7, -3, n // 2, max(n - 1, 0)])
+    return some[(np.arange(B) + r.integers(0, 7)) % 7]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Mq,n,H_q,H_kv,d_h", SHAPES)
+@pytest.mark.parametrize("lens,mode", [("all", "flat"), ("ragged", "paged"), ("edges", "flat"), ("edges", "holes")])
+def test_attention_kv4(dtype, B, Mq, n, H_q, H_kv, d_h, lens, mode):
+    r = np.random.default_rng(n + 7 * Mq)
+    check_attention(Case(n * 31 + Mq, dtype, B, Mq, n, H_q, H_kv, d_h, lens_of(lens, B, n, r), mode))
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "bf16"), ("bf16", "kv4"), ("f32", "f32"), ("f32", "kv4")])
+@pytest.mark.parametrize("B,Mq,n,H_q,H_kv,d_h", SHAPES)
+@pytest.mark.parametrize("lens,mode", [("all", "flat"), ("edges", "holes")])
+def test_attention_weights(dtype, fmt, B, Mq, n, H_q, H_kv, d_h, lens, mode):
+    r = np.random.default_rng(n + 11 * Mq)
+    check_weights(Case(n * 37 + Mq, dtype, B, Mq, n, H_q, H_kv, d_h, lens_of(lens, B, n, r), mode), fmt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Mq", [2, 40, 200])
+def test_large_scores(dtype, Mq):
+    """One key takes nearly everything: maxima that jump from block to block, exponentials that vanish."""
+    c = Case(3, dtype, 1, Mq, 150, 2, 1, 128, None, "flat", q_scale=30.0)
+    check_attention(c)
+    check_weights(c, "kv4")
+    check_weights(c, dtype)
+
+
+@pytest.mark.parametrize("Mq", [3, 150])
+def test_a_bad_query_spoils_only_itself(Mq):
+    c = Case(4, "bf16", 2, Mq, 90, 4, 2, 128)
+    q, k, v, where = c.device("kv4")
+    good = L.op_attention_kv4("bf16", q, k, v, c.rows, c.n, 4, 2, 128)
+    q[1, 2, 128:256] = float("nan")
+    got = L.op_attention_kv4("bf16", q, k, v, c.rows, c.n, 4, 2, 128)
+    assert got[1, 2, 128:256].isnan().all()
+    got[1, 2, 128:256] = good[1, 2, 128:256]
+    assert torch.equal(got, good)
+
+
+def test_a_key_that_is_there_counts_whatever_it_holds():
+    c = Case(5, "bf16", 2, 3, 90, 2, 2, 128)
+    q, k, v, where = c.device("kv4")
+    bad = torch.full((1, 256), float("nan"), dtype=torch.bfloat16, device="cuda")
+    L.op_kv4_store("bf16", bad, k, c.rows, 2, 128, rows=R.ints([90 + 17]))
+    out, lse = L.op_attention_kv4("bf16", q, k, v, c.rows, c.n, 2, 2, 128, with_lse=True)
+    assert out[0].isfinite().all() and out[1].isnan().all()
+    assert lse[0].isfinite().all() and lse[1].isnan().all()
+    w = L.op_attention_weights("bf16", "kv4", q, k, c.rows, c.n, 2, 2, 128)
+    assert w[0].isfinite().all() and w[1].isnan().all()
+
+
+# ------------------------------------------------------------------ eviction
+def check_evict(acc, keep, first, last, lens=None, row_map=None, cache_rows=None):
+    B, n = acc.shape
+    cache_rows = cache_rows or B * n
+    got = L.op_evict(R.dev(acc), keep, cache_rows, first, last, lens=None if lens is None else R.ints(lens),
+                     row_map=None if row_map is None else R.ints(row_map))
+    want = R.evict(acc, keep, R.present(B, n, cache_rows, lens, row_map), lens, n, first, last)
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy(), w, equal_nan=w.dtype == np.float32)
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 500, 1024, 1025, 4096, 5000, 17000, 70000])
+def test_evict(n):
+    r = np.random.default_rng(n)
+    B = 3 if n < 5000 else 2
+    acc = R.grid(r.exponential(1.0, (B, n)), "f32")
+    acc[0, r.random(n) < 0.5] = acc[0, 0]              # ties across the cut
+    for keep in sorted({1, (n + 1) // 2, n}):
+        last = r.integers(0, keep + 1)
+        check_evict(acc, keep, keep - last, last)
+        check_evict(acc, keep, 0, 0)
+        check_evict(acc, keep, min(4, keep), 0, lens=lens_of("edges", B, n, r))
+
+
+def test_evict_special_weights():
+    r = np.random.default_rng(1)
+    acc = r.choice(np.array([0.0, -0.0, 1.0, -1.0, np.inf, -np.inf, np.nan, 1e-42, -1e-42, 3e38], np.float32), (4, 300))
+    for keep in (1, 30, 60, 100, 150, 222, 299):
+        check_evict(acc, keep, 0, 0)
+        check_evict(acc, keep, keep // 3, keep // 4, lens=[300, 299, 40, 0])
+
+
+@pytest.mark.parametrize("n", [40, 1500, 20000])
+def test_evict_positions_that_are_not_there(n):
+    r = np.random.default_rng(n)
+    acc = R.grid(r.integers(0, 5, (3, n)), "f32")
+    rows = 4 * n
+    row_map = np.stack([r.permutation(rows)[:n] for _ in range(3)])
+    row_map[r.random((3, n)) < 0.4] = -1
+    row_map[1, : n // 2] = rows
+    row_map[2] = -7
+    for keep in (1, n // 3, n // 2, n):
+        check_evict(acc, keep, min(3, keep), 0, lens=[n, n - 3, n], row_map=row_map, cache_rows=rows)
+
+
+@pytest.mark.parametrize("fmt,H,d_h", [("f32", 2, 64), ("bf16", 3, 128), ("kv4", 3, 128), ("kv4", 1, 32), ("kv4", 2, 96), ("bf16", 1, 5),
+                                       ("f32", 1, 7)])
+@pytest.mark.parametrize("both", [True, False])
+def test_compact(fmt, H, d_h, both):
+    r = np.random.default_rng(d_h)
+    src, M, dst = 50, 30, 34
+    rows = r.permutation(src)[:M]
+    rows[[3, 7, 11, 29]] = [-1, src, 2 ** 31 - 1, -2 ** 31]
+    def tensor(count, seed):
+        x = R.grid(np.random.default_rng(seed).standard_normal((count, H * d_h)), "bf16")
+        if fmt != "kv4":
+            return R.dev(x, fmt)
+        c = torch.zeros(L.kv4_bytes(count, H, d_h), dtype=torch.uint8, device="cuda")
+        L.op_kv4_store("f32", R.dev(x), c, count, H, d_h)
+        return c
+    def values(t, count):
+        return host(L.op_kv4_load("f32", t, count, H, d_h)) if fmt == "kv4" else host(t)
+    k, v, kd, vd = tensor(src, 1), tensor(src, 2), tensor(dst, 3), tensor(dst, 4)
+    want = [values(kd, dst), values(vd, dst)]
+    for w, s in zip(want, (values(k, src), values(v, src))):
+        for i, row in enumerate(rows):
+            if 0 <= row < src:
+                w[i] = s[row]
+    if not both:
+        want[1] = values(vd, dst)
+    L.op_compact(fmt, R.ints(rows), src, H, d_h, k, kd, *((v, vd) if both else ()), dst_rows=dst)
+    assert np.array_equal(values(kd, dst), want[0]) and np.array_equal(values(vd, dst), want[1])
+
+
+# ------------------------------------------------------------------ 8-bit linear maps
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 1), (3, 127), (5, 128), (9, 129), (2, 1000), (4, 4096), (3, 8193), (2, 18944)])
+def test_quant8(dtype, M, K):
+    r = np.random.default_rng(K)
+    x = R.grid(r.standard_normal((M + 4, K)) * 10.0 ** r.uniform(-6, 6, (M + 4, 1)), dtype).copy()
+    x[0, : K // 2] = x[0, 0] if x[0, 0] else 1.0
+    x[M] = 0.0
+    x[M + 1] = 2.0 ** -119
+    x[M + 2, 0], x[M + 3, -1] = np.inf, np.nan
+    idx = r.permutation(M + 4)
+    for rows in (None, idx):
+        got, scale = L.op_quant8(dtype, R.dev(x, dtype), row_idx=None if rows is None else R.ints(rows))
+        q, s = R.quant8(x if rows is None else x[rows])
+        assert np.array_equal(scale.cpu().numpy(), s, equal_nan=True)
+        got = got.cpu().numpy()
+        assert np.array_equal(got[:, :K], q) and (got[:, K:] == 0).all()
+
+
+def check_linear(dtype, M, N, K, seed=0, extreme=False):
+    r = np.random.default_rng(M + 3 * N + 7 * K + seed)
+    kp = L.i8_row_bytes(K)
+    a, w = np.zeros((M, kp), np.int8), np.zeros((N, kp), np.int8)
+    a[:, :K] = r.integers(-127, 128, (M, K)) if not extreme else 127
+    w[:, :K] = r.integers(-127, 128, (N, K)) if not extreme else -127
+    sa, sw = (R.grid(r.uniform(0.001, 0.1, m), "f32") for m in (M, N))
+    sa[M // 2] = 0.0
+    got = L.op_linear_i8(dtype, torch.from_numpy(a).cuda(), R.dev(sa), torch.from_numpy(w).cuda(), R.dev(sw), K)
+    # integer sums below 2^53 are exact in float64
+    sums = torch.from_numpy(a).cuda().double() @ torch.from_numpy(w).cuda().double().t()
+    want = (sums.cpu().numpy() * sa.astype(np.float64)[:, None]) * sw.astype(np.float64)
+    # the sum as float32, two products, the result's rounding
+    tol = np.abs(want) * (3 * 2.0 ** -24 + (R.HALF_STEP["bf16"] if dtype == "bf16" else 0.0)) * 1.0001
+    err = np.abs(host(got) - want)
+    assert (err <= tol).all(), (err - tol).max()
+
+
+LINEAR = [(1, 1, 1), (1, 256, 256), (3, 17, 100), (16, 64, 128), (17, 65, 129), (64, 1000, 1024), (65, 129, 257), (100, 512, 4096),
+          (128, 384, 640), (200, 333, 1111), (256, 256, 512), (300, 1030, 384), (513, 260, 900), (33, 4096, 2048), (1, 5000, 4096),
+          (700, 520, 1280)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", LINEAR)
+def test_linear_i8(dtype, M, N, K):
+    check_linear(dtype, M, N, K)
+
+
+def test_linear_i8_longest_contraction():
+    check_linear("f32", 3, 5, 131072, extreme=True)     # 127 * 127 * 2^17 is just inside an int32
+
+
+def test_linear_i8_nan_scale_stays_in_its_row():
+    x = R.grid(np.random.default_rng(8).standard_normal((40, 200)), "bf16").copy()
+    x[7, 5] = np.inf
+    a, sa = L.op_quant8("bf16", R.dev(x, "bf16"))
+    w, sw = L.op_quant8("bf16", R.dev(np.where(np.isfinite(x[:30]), x[:30], 0), "bf16"))
+    out = L.op_linear_i8("bf16", a, sa, w, sw, 200)
+    assert out[7].isnan().all() and out[:7].isfinite().all() and out[8:].isfinite().all()
