@@ -410,7 +410,8 @@ int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int3
 /* Cached keys of the operations below: sequence b has the positions j < lens[b] (n if lens is NULL; values outside [0, n] count
  * as the nearest of the two), position j in cache row row_map[b * n + j] (b * n + j if row_map is NULL).  A position whose entry is
  * no row of the cache is not there.  What lies in rows and positions that are not there has no influence whatever it
- * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements.
+ * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements; at most 2^24 positions and 2^23 rows of B * Mq *
+ * H_q.
  *
  * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
  * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without

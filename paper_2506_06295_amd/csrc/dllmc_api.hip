@@ -1161,6 +1161,7 @@ inline size_t elem_bytes(int32_t dtype) { return dtype == DLLMC_BF16 ? 2 : 4; }
 
 constexpr int kMaxRows = 1 << 24;  // rows of a cache, positions of a batch (as for a context)
 constexpr int kMaxWidth = 1 << 16;  // H * d_h
+constexpr int kMaxBatch = 1 << 16;   // (a launch has at most 2^32 work-items)
 constexpr int kMaxI8K = 1 << 17;   // 127 * 127 * 2^17 < 2^31: a whole contraction fits an int32 sum
 
 bool kv4_shape_ok(int32_t rows, int32_t H, int32_t d_h) {
@@ -1172,7 +1173,7 @@ bool attend_shape_ok(int32_t B, int32_t Mq, int32_t cache_rows, const int32_t* r
                      int32_t H_kv, int32_t d_h) {
   if (B < 1 || Mq < 1 || n < 1 || H_kv < 1 || H_q < H_kv || H_q % H_kv || (d_h != 64 && d_h != 128 && d_h != 256)) return false;
   if (cache_rows < 1 || cache_rows > kMaxRows || n > kMaxRows / B || H_q > kMaxWidth / d_h || Mq > kMaxRows / B) return false;
-  if (static_cast<long long>(B) * Mq * H_q > (1ll << 30)) return false;
+  if (B > kMaxBatch || static_cast<long long>(B) * Mq * H_q > (1ll << 23)) return false;
   if (row_map == nullptr && static_cast<long long>(B) * n > cache_rows) return false;
   return aligned4(row_map) && aligned4(lens);
 }
@@ -1291,7 +1292,7 @@ int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* 
 int dllmc_op_evict(const float* acc, int32_t B, int32_t n, const int32_t* lens, const int32_t* row_map, int32_t cache_rows,
                    int32_t keep, int32_t first, int32_t last, int32_t* kept, int32_t* kept_rows, int32_t* new_lens, float* acc_out,
                    void* hip_stream) {
-  if (!acc || !kept || !kept_rows || !new_lens || B < 1 || n < 1 || n > kMaxRows / B || cache_rows < 1 || cache_rows > kMaxRows ||
+  if (!acc || !kept || !kept_rows || !new_lens || B < 1 || B > kMaxBatch || n < 1 || n > kMaxRows / B || cache_rows < 1 || cache_rows > kMaxRows ||
       keep < 1 || keep > n || first < 0 || last < 0 || first > keep || last > keep - first || !aligned4(acc) || !aligned4(lens) ||
       !aligned4(row_map) || !aligned4(kept) || !aligned4(kept_rows) || !aligned4(new_lens) || !aligned4(acc_out) ||
       (row_map == nullptr && static_cast<long long>(B) * n > cache_rows))
@@ -1342,7 +1343,7 @@ size_t dllmc_i8_row_bytes(int32_t K) { return K >= 1 && K <= kMaxI8K ? i8_row_by
 
 int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
                     void* hip_stream) {
-  if (!dtype_ok(dtype) || !x || !q || !scale || M < 1 || M > kMaxRows || K < 1 || K > kMaxI8K || !aligned16(q) || !aligned4(scale) ||
+  if (!dtype_ok(dtype) || !x || !q || !scale || M < 1 || M >= kMaxRows || K < 1 || K > kMaxI8K || !aligned16(q) || !aligned4(scale) ||
       !aligned4(row_idx) || reinterpret_cast<uintptr_t>(x) % elem_bytes(dtype))
     return DLLMC_EINVAL;
   const size_t qb = M * i8_row_bytes(K), sb = static_cast<size_t>(M) * 4;

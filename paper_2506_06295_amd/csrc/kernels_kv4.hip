@@ -201,20 +201,6 @@ void launch_kv4_load(int dtype, Kv4Tensor c, int cache_rows, int d_h, const int*
                        static_cast<float*>(out));
 }
 
-size_t attention_kv4_scratch_bytes(int, int, int, int, int, int, int) { return 0; }
-
-void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
-                          int H_kv, int d_h, void* out, float* lse, void*, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(static_cast<long long>(B) * Mq * H_q));
-  const size_t lds = (d_h + 64) * sizeof(float);
-  if (dtype == 1)
-    hipLaunchKernelGGL((k_attend_simple<bf16_t, Kv4Tensor>), grid, dim3(64), lds, st, static_cast<const bf16_t*>(q), Mq, k, v, keys,
-                       H_q, H_kv, d_h, static_cast<bf16_t*>(out), lse);
-  else
-    hipLaunchKernelGGL((k_attend_simple<float, Kv4Tensor>), grid, dim3(64), lds, st, static_cast<const float*>(q), Mq, k, v, keys, H_q,
-                       H_kv, d_h, static_cast<float*>(out), lse);
-}
-
 size_t attention_weights_scratch_bytes(int, int, int B, int Mq, int, int H_q, int, int) {
   return static_cast<size_t>(B) * Mq * H_q * sizeof(float);
 }
