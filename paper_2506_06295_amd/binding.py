@@ -225,7 +225,8 @@ def _check(rc: int, what: str) -> None:
 
 
 def _stream_handle() -> int:
-    return int(torch.cuda.current_stream().cuda_stream)
+    # (the handle alone: 0.3 us, torch.cuda.current_stream().cuda_stream makes an object for 3)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -547,12 +548,12 @@ def op_attention(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
 
 
 # ---- the step's pieces in fewer bits ------------------------------------------------------------
-def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
+def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple) -> Optional[int]:
     """Address of a contiguous tensor of the current device, this dtype and shape (None stays None)."""
     if t is None:
         return None
-    if not (t.is_cuda and t.device.index == torch.cuda.current_device() and t.is_contiguous() and t.dtype == dtype
-            and tuple(t.shape) == tuple(shape)):
+    d = t.get_device()
+    if d < 0 or d != torch.cuda.current_device() or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise DllmcError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
     return t.data_ptr()

@@ -13,36 +13,9 @@ namespace dllmc {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
-
-template <typename T> struct Parts;  // bf16 parts of a query element and of a probability
-template <> struct Parts<bf16_t> { static constexpr int kQ = 1, kP = 2; };
-template <> struct Parts<float> { static constexpr int kQ = 3, kP = 3; };
-
-// Eight query elements as bf16 parts: x = part 0 + part 1 + part 2, each what is left rounded.
-template <int D>
-__device__ __forceinline__ void load_query(const bf16_t* p, bf16x8 (&f)[1]) {
-  f[0] = *reinterpret_cast<const bf16x8*>(p);
-}
-template <int D>
-__device__ __forceinline__ void load_query(const float* p, bf16x8 (&f)[3]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int u = 0; u < 3; ++u) {
-    uint32_t w[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      w[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
-      x[2 * t] -= __uint_as_float(w[t] << 16);
-      x[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
-    }
-    f[u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-  }
-}
 
 // A block of 32 keys as a wavefront loads it.  K: lane (ln, lg) has elements lg D/4 .. + D/4 of keys ln and 16 + ln (any deal of
 // the elements to the contraction will do that the queries share; this one makes a load of 16 keys one run of memory).  V: piece
@@ -274,7 +247,7 @@ __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const A
     for (int i = 0; i < QB; ++i) {
       const T* p = q + row_at(r0 + i * 16 + ln) * D + lg * (D / 4);
 #pragma unroll
-      for (int c = 0; c < C; ++c) load_query<D>(p + 8 * c, qf[i][c]);
+      for (int c = 0; c < C; ++c) load_query(p + 8 * c, qf[i][c]);
     }
     for (; blk + 4 < blk1; blk += 8) {
       ld.fetch((blk + 4) * 32, rk, b1);
@@ -338,7 +311,7 @@ __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const A
         for (int e = 0; e < E; e += 4)
           *reinterpret_cast<float4*>(out + w * D + t + e) = make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
       }
-      if (lse != nullptr && t == 0) lse[w] = (M + log2f(L)) * 0.6931471805599453f;
+      if (lse != nullptr && t == 0) lse[w] = (M + log2f(L)) * kLn2;
     } else {
 #pragma unroll
       for (int e = 0; e < E; e += 4)
@@ -348,8 +321,10 @@ __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const A
   }
 }
 
+// workgroups per CU that its registers leave room for without spilling
+constexpr int few_groups(bool f32, int D, int QB) { return D == 256 ? (f32 ? 1 : 2) : QB == 1 ? (f32 ? 2 : 3) : QB == 2 ? 2 : 1; }
 template <typename T, int D, int QB, bool PAGED>
-__global__ __launch_bounds__(256, QB == 1 ? 3 : QB == 2 ? 2 : 1) void k_attend_few(const T* __restrict__ q, AttendShape s, CacheView k, CacheView v,
+__global__ __launch_bounds__(256, few_groups(sizeof(T) == 4, D, QB)) void k_attend_few(const T* __restrict__ q, AttendShape s, CacheView k, CacheView v,
                                                                           Keys keys, T* __restrict__ out, float* __restrict__ lse,
                                                                           float* __restrict__ part, float2* __restrict__ part_ml) {
   // row tiles of one head and range run side by side: they read the same keys
@@ -388,14 +363,14 @@ __global__ __launch_bounds__(256) void k_attend_merge(const float* __restrict__ 
   const float inv = L == 0.f ? 0.f : 1.0f / L;
 #pragma unroll
   for (int e = 0; e < E; ++e) stf(out + w * D + lane * E + e, o[e] * inv);
-  if (lse != nullptr && lane == 0) lse[w] = (M + log2f(L)) * 0.6931471805599453f;
+  if (lse != nullptr && lane == 0) lse[w] = (M + log2f(L)) * kLn2;
 }
 
 struct AttendPlan { int QB, tiles, KS, per; };
-AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv) {
+AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
   const int NR = Mq * (H_q / H_kv), nblk = (n + 31) / 32;
   AttendPlan p{};
-  p.QB = NR <= 16 || dtype == 0 ? 1 : NR <= 32 ? 2 : 4;
+  p.QB = NR <= 16 || dtype == 0 || d_h == 256 ? 1 : NR <= 32 ? 2 : 4;
   p.tiles = (NR + 16 * p.QB - 1) / (16 * p.QB);
   const long long items = static_cast<long long>(B) * H_kv * p.tiles;
   const long long want = p.QB == 4 ? 256 : 512;
@@ -411,13 +386,13 @@ AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv) {
 }  // namespace
 
 size_t attention_kv4_scratch_bytes(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
-  const AttendPlan p = plan_attend(dtype, B, Mq, n, H_q, H_kv);
+  const AttendPlan p = plan_attend(dtype, B, Mq, n, H_q, H_kv, d_h);
   return p.KS == 1 ? 0 : static_cast<size_t>(B) * Mq * H_q * p.KS * (d_h + 2) * sizeof(float);
 }
 
 void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
                           int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st) {
-  const AttendPlan p = plan_attend(dtype, B, Mq, keys.n, H_q, H_kv);
+  const AttendPlan p = plan_attend(dtype, B, Mq, keys.n, H_q, H_kv, d_h);
   const AttendShape s{Mq, H_q, H_kv, H_q / H_kv, Mq * (H_q / H_kv), p.tiles, p.KS, p.per};
   const long long rows = static_cast<long long>(B) * Mq * H_q;
   float* part = static_cast<float*>(scratch);
@@ -434,7 +409,7 @@ void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheVi
                          rows, static_cast<T*>(out), lse);
   };
   auto with_qb = [&](auto t, auto d, auto paged) {
-    if constexpr (sizeof(t) == 4) go(t, d, std::integral_constant<int, 1>{}, paged);
+    if constexpr (sizeof(t) == 4 || decltype(d)::value == 256) go(t, d, std::integral_constant<int, 1>{}, paged);
     else if (p.QB == 1) go(t, d, std::integral_constant<int, 1>{}, paged);
     else if (p.QB == 2) go(t, d, std::integral_constant<int, 2>{}, paged);
     else go(t, d, std::integral_constant<int, 4>{}, paged);

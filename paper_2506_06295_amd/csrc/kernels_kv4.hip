@@ -92,86 +92,6 @@ __global__ __launch_bounds__(256) void k_kv4_load(Kv4Tensor c, int cache_rows, i
   }
 }
 
-// ---- attention, one wavefront per query and head --------------------------------------------------------
-// Scores twice: once for the maximum and the sum, once for the probabilities of 64 keys at a time.
-template <typename T, typename C>
-__device__ __forceinline__ float score(const float* qs, const CacheView& c, int h, int row, int d_h) {
-  float s = 0.f;
-  for (int t = 0; t < d_h; ++t) s = fmaf(qs[t], cache_at<C>(c, h, row, t, d_h), s);
-  return s;
-}
-
-template <typename T, typename C>
-__global__ __launch_bounds__(64) void k_attend_simple(const T* __restrict__ q, int Mq, CacheView kc, CacheView vc, Keys keys,
-                                                      int H_q, int H_kv, int d_h, T* __restrict__ out, float* __restrict__ lse) {
-  extern __shared__ float sm[];
-  float* qs = sm;
-  float* ps = sm + d_h;
-  const int lane = threadIdx.x;
-  const long long w = blockIdx.x;
-  const int a = static_cast<int>(w % H_q), i = static_cast<int>(w / H_q % Mq), b = static_cast<int>(w / H_q / Mq);
-  const int h = a / (H_q / H_kv), len = keys.length(b);
-  const T* qr = q + w * d_h;
-  const float scale = 1.0f / sqrtf(static_cast<float>(d_h));
-  for (int t = lane; t < d_h; t += 64) qs[t] = ldf(qr + t) * scale;
-  __syncthreads();
-  float m = -INFINITY, l = 0.f;
-  for (int j = lane; j < len; j += 64) {
-    const int row = keys.row(b, j);
-    if (row < 0) continue;
-    const float s = score<T, C>(qs, kc, h, row, d_h), top = fmaxf(m, s);
-    const float u = top == -INFINITY ? 0.f : top;
-    l = l * expf(m - u) + expf(s - u);
-    m = top;
-  }
-  const float M = wave_max(m), U = M == -INFINITY ? 0.f : M;
-  const float L = wave_sum(l * expf(m - U));
-  if (lse != nullptr && lane == 0) lse[w] = M + logf(L);
-  if (out == nullptr) return;
-  float o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j0 = 0; j0 < len; j0 += 64) {
-    const int j = j0 + lane, mine = j < len ? keys.row(b, j) : -1;
-    __syncthreads();
-    ps[lane] = mine >= 0 ? expf(score<T, C>(qs, kc, h, mine, d_h) - U) : 0.f;
-    __syncthreads();
-    for (int e = 0; e < 64 && j0 + e < len; ++e) {
-      const int row = keys.row(b, j0 + e);
-      if (row < 0) continue;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (lane + 64 * t < d_h) o[t] = fmaf(ps[e], cache_at<C>(vc, h, row, lane + 64 * t, d_h), o[t]);
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (lane + 64 * t < d_h) stf(out + w * d_h + lane + 64 * t, L == 0.f ? 0.f : o[t] / L);
-  (void)i;
-}
-
-// acc_out[b][j] = acc_in[b][j] + sum over queries and heads of exp(s - lse): a wavefront takes 64 keys
-template <typename T, typename C>
-__global__ __launch_bounds__(64) void k_weigh_simple(const T* __restrict__ q, int Mq, CacheView kc, Keys keys, int H_q, int H_kv,
-                                                     int d_h, const float* __restrict__ lse, const float* __restrict__ acc_in,
-                                                     float* __restrict__ acc_out) {
-  extern __shared__ float sm[];
-  const int tiles = (keys.n + 63) / 64, lane = threadIdx.x;
-  const int b = blockIdx.x / tiles, j = blockIdx.x % tiles * 64 + lane;
-  const int row = j < keys.length(b) ? keys.row(b, j) : -1;
-  const float scale = 1.0f / sqrtf(static_cast<float>(d_h));
-  float sum = 0.f;
-  for (int r = 0; r < Mq * H_q; ++r) {
-    const long long w = static_cast<long long>(b) * Mq * H_q + r;
-    __syncthreads();
-    for (int t = lane; t < d_h; t += 64) sm[t] = ldf(q + w * d_h + t) * scale;
-    __syncthreads();
-    if (row >= 0) sum += expf(score<T, C>(sm, kc, r % H_q / (H_q / H_kv), row, d_h) - lse[w]);
-  }
-  if (j < keys.n) {
-    const size_t at = static_cast<size_t>(b) * keys.n + j;
-    acc_out[at] = (acc_in ? acc_in[at] : 0.f) + sum;
-  }
-}
-
 inline unsigned groups(long long items) {
   const long long g = (items + 255) / 256;
   return static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20);
@@ -199,35 +119,6 @@ void launch_kv4_load(int dtype, Kv4Tensor c, int cache_rows, int d_h, const int*
   else
     hipLaunchKernelGGL(k_kv4_load<float>, dim3(groups(pieces)), dim3(256), 0, st, c, cache_rows, d_h, rows, pieces, width,
                        static_cast<float*>(out));
-}
-
-size_t attention_weights_scratch_bytes(int, int, int B, int Mq, int, int H_q, int, int) {
-  return static_cast<size_t>(B) * Mq * H_q * sizeof(float);
-}
-
-void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
-                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
-                              hipStream_t st) {
-  const dim3 rows(static_cast<unsigned>(static_cast<long long>(B) * Mq * H_q)), tiles(B * ((keys.n + 63) / 64));
-  const size_t lds = (d_h + 64) * sizeof(float);
-  float* own = static_cast<float*>(scratch);
-  auto go = [&](auto t, auto c) {
-    typedef decltype(t) T;
-    typedef decltype(c) C;
-    if (lse == nullptr)
-      hipLaunchKernelGGL((k_attend_simple<T, C>), rows, dim3(64), lds, st, static_cast<const T*>(q), Mq, k, k, keys, H_q, H_kv, d_h,
-                         static_cast<T*>(nullptr), own);
-    hipLaunchKernelGGL((k_weigh_simple<T, C>), tiles, dim3(64), lds, st, static_cast<const T*>(q), Mq, k, keys, H_q, H_kv, d_h,
-                       lse ? lse : own, acc_in, acc_out);
-  };
-  if (format == 2) {
-    if (dtype == 1) go(bf16_t(), Kv4Tensor());
-    else go(float(), Kv4Tensor());
-  } else if (dtype == 1) {
-    go(bf16_t(), bf16_t());
-  } else {
-    go(float(), float());
-  }
 }
 
 }  // namespace dllmc

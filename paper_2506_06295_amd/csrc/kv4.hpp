@@ -60,15 +60,30 @@ __device__ __forceinline__ bf16x8 kv4_expand(uint32_t w, uint32_t scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// element t of a cached row's head h
-template <typename C> __device__ __forceinline__ float cache_at(const CacheView& c, int h, int row, int t, int d_h) {
-  return ldf(static_cast<const C*>(c.rows) + (static_cast<size_t>(row) * c.H + h) * d_h + t);
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <typename T> struct Parts;  // bf16 parts of a query element and of a probability
+template <> struct Parts<bf16_t> { static constexpr int kQ = 1, kP = 2; };
+template <> struct Parts<float> { static constexpr int kQ = 3, kP = 3; };
+
+// Eight query elements as bf16 parts: x = part 0 + part 1 + part 2, each what is left rounded.
+__device__ __forceinline__ void load_query(const bf16_t* p, bf16x8 (&f)[1]) {
+  f[0] = *reinterpret_cast<const bf16x8*>(p);
 }
-template <> __device__ __forceinline__ float cache_at<Kv4Tensor>(const CacheView& c, int h, int row, int t, int d_h) {
-  const size_t at = static_cast<size_t>(h) * c.cache_rows + row;
-  const uint32_t byte = c.kv4.codes[at * (d_h / 2) + t / 2], scale = c.kv4.scales[at * (d_h / 32) + t / 32];
-  const uint4 v = __builtin_bit_cast(uint4, kv4_expand(byte, scale));
-  return __uint_as_float(t % 2 ? v.x & 0xffff0000u : v.x << 16);
+__device__ __forceinline__ void load_query(const float* p, bf16x8 (&f)[3]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    uint32_t w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      w[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
+      x[2 * t] -= __uint_as_float(w[t] << 16);
+      x[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
+    }
+    f[u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+  }
 }
 
 void launch_kv4_store(int dtype, const void* x, int M, int width, const int* rows, Kv4Tensor c, int cache_rows, int d_h,
