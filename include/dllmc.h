@@ -454,7 +454,7 @@ size_t dllmc_i8_row_bytes(int32_t K);
 int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
                     void* hip_stream);
 /* out[i][j] = a_scale[i] * w_scale[j] * (sum over k of a[i][k] * w[j][k], in integers), [M, N] of dtype; a and w as dllmc_op_quant8
- * leaves them.  scratch: at least dllmc_op_linear_i8_scratch_bytes() bytes, which may be 0.  Bit-reproducible. */
+ * leaves them, M <= 2^22, N <= 2^24.  scratch: at least dllmc_op_linear_i8_scratch_bytes() bytes, which may be 0.  Bit-reproducible. */
 size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K);
 int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int32_t M, const int8_t* w,
                        const float* w_scale, int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes,

@@ -1162,6 +1162,7 @@ inline size_t elem_bytes(int32_t dtype) { return dtype == DLLMC_BF16 ? 2 : 4; }
 constexpr int kMaxRows = 1 << 24;  // rows of a cache, positions of a batch (as for a context)
 constexpr int kMaxWidth = 1 << 16;  // H * d_h
 constexpr int kMaxBatch = 1 << 16;   // (a launch has at most 2^32 work-items)
+constexpr int kMaxI8M = 1 << 22;     // (row tiles in y: at most 2^16)
 constexpr int kMaxI8K = 1 << 17;   // 127 * 127 * 2^17 < 2^31: a whole contraction fits an int32 sum
 
 bool kv4_shape_ok(int32_t rows, int32_t H, int32_t d_h) {
@@ -1359,13 +1360,13 @@ int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_
 }
 
 size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K) {
-  if (M < 1 || M > kMaxRows || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return 0;
+  if (M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return 0;
   return linear_i8_scratch_bytes(M, N, K);
 }
 
 int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int32_t M, const int8_t* w, const float* w_scale,
                        int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes, void* hip_stream) {
-  if (!dtype_ok(dtype) || !a || !a_scale || !w || !w_scale || !out || M < 1 || M > kMaxRows || N < 1 || N > kMaxRows || K < 1 ||
+  if (!dtype_ok(dtype) || !a || !a_scale || !w || !w_scale || !out || M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 ||
       K > kMaxI8K || !aligned16(a) || !aligned16(w) || !aligned4(a_scale) || !aligned4(w_scale) ||
       reinterpret_cast<uintptr_t>(out) % elem_bytes(dtype) || !aligned16(scratch))
     return DLLMC_EINVAL;

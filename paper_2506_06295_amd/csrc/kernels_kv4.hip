@@ -15,25 +15,6 @@ namespace {
 // ---- rows in and out -------------------------------------------------------------------------------
 // Four lanes take a block, eight elements each: one 16-byte load of bf16 (two of float32), a maximum over the quad
 // by lane moves, four bytes of codes.  Bound by the bytes: 64.5 bits an element in and out of a bf16 row.
-template <typename T> struct Eight;
-template <> struct Eight<float> {
-  static __device__ __forceinline__ void load(const float* p, float (&x)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-};
-template <> struct Eight<bf16_t> {
-  static __device__ __forceinline__ void load(const bf16_t* p, float (&x)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      x[2 * t] = __uint_as_float(w[t] << 16);
-      x[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
-    }
-  }
-};
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_kv4_store(const T* __restrict__ x, long long pieces, int width,
                                                    const int* __restrict__ rows, Kv4Tensor c, int cache_rows, int d_h) {

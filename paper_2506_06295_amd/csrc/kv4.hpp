@@ -60,6 +60,26 @@ __device__ __forceinline__ bf16x8 kv4_expand(uint32_t w, uint32_t scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// eight neighbouring elements of a 16-byte aligned row as float32
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  static __device__ __forceinline__ void load(const float* p, float (&x)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
+template <> struct Eight<bf16_t> {
+  static __device__ __forceinline__ void load(const bf16_t* p, float (&x)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      x[2 * t] = __uint_as_float(w[t] << 16);
+      x[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+    }
+  }
+};
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <typename T> struct Parts;  // bf16 parts of a query element and of a probability
