@@ -326,6 +326,11 @@ int32_t dllmc_plan_vverify(int32_t dtype, int32_t rows, int32_t d, int32_t d_kv)
  * d_q, heads of 128, 3: V-verify of N = d_kv columns.  *cols (may be NULL): the tile's columns (gate/up: of each matrix). */
 int32_t dllmc_plan_tile(int32_t launch, int32_t M, int32_t N, int32_t N0, int32_t K, int32_t* cols);
 
+/* Host-only: rows of the tiles that dllmc_op_linear_i8 takes; *cols (may be NULL) their columns, *slices the slices of the contraction
+ * (more than one: a launch adds them), *whole 1: the contraction of a tile is walked by wavefronts of a quarter of the tile each, 0:
+ * wavefronts share it. */
+int32_t dllmc_plan_linear_i8(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole);
+
 /* Host-only: the number of key ranges of a bf16 attention of Mq < 128 queries per sequence with head width 128
  * (split_keys: with a scratch buffer).  *queries (may be NULL): queries per workgroup of the kernel whose
  * wavefronts split the keys, 16, 32 or 64; 0: 64 queries whose wavefronts walk all keys together; -1: the

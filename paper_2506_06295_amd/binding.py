@@ -36,6 +36,7 @@ EXPORTS = (
     "dllmc_kv4_bytes", "dllmc_op_kv4_store", "dllmc_op_kv4_load", "dllmc_op_attention_kv4_scratch_bytes",
     "dllmc_op_attention_kv4", "dllmc_op_attention_weights_scratch_bytes", "dllmc_op_attention_weights", "dllmc_op_evict",
     "dllmc_op_compact", "dllmc_i8_row_bytes", "dllmc_op_quant8", "dllmc_op_linear_i8_scratch_bytes", "dllmc_op_linear_i8",
+    "dllmc_plan_linear_i8",
 )
 NUM_KERNEL_CLASSES = 13
 
@@ -209,6 +210,7 @@ def lib() -> C.CDLL:
                 ("dllmc_i8_row_bytes", size, [i32]),
                 ("dllmc_op_quant8", C.c_int, [i32, ptr, ptr, i32, i32, ptr, ptr, ptr]),
                 ("dllmc_op_linear_i8_scratch_bytes", size, [i32] * 3),
+                ("dllmc_plan_linear_i8", i32, [i32] * 3 + [C.POINTER(i32)] * 3),
                 ("dllmc_op_linear_i8", C.c_int, [i32, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, size, ptr])):
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -682,6 +684,15 @@ def i8_row_bytes(K: int) -> int:
     if n == 0:
         raise DllmcError(f"dllmc_i8_row_bytes: no 8-bit rows of {K}")
     return n
+
+
+def plan_linear_i8(M: int, N: int, K: int):
+    """(rows, columns) of op_linear_i8's tiles, slices of the contraction, whether it takes the tile kernels; no GPU needed."""
+    cols, slices, whole = C.c_int32(), C.c_int32(), C.c_int32()
+    rows = lib().dllmc_plan_linear_i8(M, N, K, C.byref(cols), C.byref(slices), C.byref(whole))
+    if rows < 1:
+        raise DllmcError("dllmc_plan_linear_i8: invalid argument")
+    return (rows, cols.value), slices.value, bool(whole.value)
 
 
 def op_quant8(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = None):

@@ -1359,6 +1359,15 @@ int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_
   return DLLMC_OK;
 }
 
+int32_t dllmc_plan_linear_i8(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole) {
+  if (M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return DLLMC_EINVAL;
+  const I8Plan p = plan_i8(M, N, static_cast<int>(i8_row_bytes(K)));
+  if (cols) *cols = p.bn;
+  if (slices) *slices = p.S;
+  if (whole) *whole = p.wide;
+  return p.bm;
+}
+
 size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K) {
   if (M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return 0;
   return linear_i8_scratch_bytes(M, N, K);

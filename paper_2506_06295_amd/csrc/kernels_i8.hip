@@ -129,7 +129,7 @@ template <int RG, int RB, int NB> struct I8Ring {
   static constexpr int T = R / 8 * SS, L = T / 8, LR = T % 8;  // load instructions of a stage, per wavefront, one more for the first LR
 };
 
-template <typename T, int RG, int RB, int NB, bool NT>
+template <typename T, int RG, int RB, int NB>
 __device__ __forceinline__ void i8_ring_body(const int8_t* __restrict__ A, const float* __restrict__ sa, int M,
                                              const int8_t* __restrict__ W, const float* __restrict__ sw, int N, int Kp, int per_slice,
                                              T* __restrict__ out, int* __restrict__ sums) {
@@ -164,11 +164,7 @@ __device__ __forceinline__ void i8_ring_body(const int8_t* __restrict__ A, const
   auto issue_one = [&](int stage, int kt, int j) {
     const int q = wave + 8 * j;
     const int line = min(kt * SS + sub[j], lines - 1);  // (columns past the last one repeat it and are not multiplied)
-    const bool weight = q % (R / 8) * 8 >= BM;
-    if (NT && weight)
-      __builtin_amdgcn_global_load_lds(src[j] + line * 128, &lds[stage][q * 64], 16, 0, 2);
-    else
-      __builtin_amdgcn_global_load_lds(src[j] + line * 128, &lds[stage][q * 64], 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(src[j] + line * 128, &lds[stage][q * 64], 16, 0, 0);
   };
   auto issue = [&](int stage, int kt) {
     const int k = kt + rot < nkt ? kt + rot : kt + rot - nkt;
@@ -262,11 +258,11 @@ __device__ __forceinline__ void i8_ring_body(const int8_t* __restrict__ A, const
   }
 }
 
-template <typename T, int RG, int RB, int NB, bool NT>
+template <typename T, int RG, int RB, int NB>
 __global__ __launch_bounds__(512) void k_i8_ring(const int8_t* __restrict__ A, const float* __restrict__ sa, int M,
                                                  const int8_t* __restrict__ W, const float* __restrict__ sw, int N, int Kp,
                                                  int per_slice, T* __restrict__ out, int* __restrict__ sums) {
-  i8_ring_body<T, RG, RB, NB, NT>(A, sa, M, W, sw, N, Kp, per_slice, out, sums);
+  i8_ring_body<T, RG, RB, NB>(A, sa, M, W, sw, N, Kp, per_slice, out, sums);
 }
 
 // out = scaled sum of S slices
@@ -481,18 +477,25 @@ __global__ __launch_bounds__(256, 1) void k_i8_wide(const int8_t* __restrict__ A
   i8_wide_body<T, WM, WN, MI, NJ>(A, sa, M, W, sw, N, Kp, out);
 }
 
-struct I8Plan { int wide, bm, bn, S, per; };  // wide: tile kernel; else ring of bm x bn and S slices of `per` bytes
-I8Plan plan_i8(int M, int N, int Kp) {
-  if (M > 128) {
-    if (M > 2048) return {1, 256, 256, 1, Kp};
-    return {1, 128, 128, 1, Kp};
-  }
-  const int bm = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-  int nb = 1;
-  while (nb < 4 && (N + 16 * nb - 1) / (16 * nb) > 256) ++nb;
-  return {0, bm, 16 * nb, 1, Kp};
-}
-
+// Tile and slices with the lowest estimate, us: start + rounds of 256 workgroups x (round + line x 128-byte columns) + MB of weights x
+// w + MB of results x out, or of int32 sums x sums + the launch that adds them.  Fitted (9 % rms) to 4500 launches, cold
+// weights, 1 to 12288 rows, nine maps of 256 to 18944; the choices are 1.1 % from the quickest shape on average, and the shapes
+// left out of the list (ring 32 x 32, 64 x 32, 128 x 16 and x 32, tiles 64 x 128 and x 256) not 0.1 % more.  Floors: 64 rows x 12288 x 4096
+// 10.5 us of bytes, 15.0 reached (a workgroup takes in 64 rows besides its 48 of the weights: 450 KB a CU at 40 GB/s); one row 10.1 and 10.8;
+// 12288 rows 526 at the rate of a large library product, 509.  Non-temporal weights: 3 % quicker cold up to 16 rows, 6 % slower from a
+// cache, and slower with more rows: not taken.
+struct I8Cost { int wide, bm, bn; double start, round, line, w, out, sums, add; };
+constexpr I8Cost kI8Costs[] = {
+    {0, 16, 16, 1.41, 1.34, 0.068, 0.0501, 3.8, 0.705, 3},      {0, 16, 32, 1.52, 1.41, 0.08, 0.0747, 2.2, 0.656, 3.04},
+    {0, 16, 48, 1.69, 1.62, 0.104, 0.0634, 1.56, 0.307, 3.26},  {0, 16, 64, 1.81, 1.74, 0.126, 0.0901, 0.233, 0.467, 2.5},
+    {0, 32, 16, 1.53, 1.15, 0.148, 0.0137, 2, 0.987, 2.89},     {0, 32, 48, 2.31, 1.85, 0.164, 0.0556, 0.0428, 0.286, 2.23},
+    {0, 32, 64, 1.96, 1.1, 0.179, 0.059, 0.899, 0.753, 2.69},   {0, 64, 16, 2.74, 0.453, 0.172, 0.051, 1.24, 0.534, 2.83},
+    {0, 64, 48, 2.38, 1.27, 0.295, 0.0213, 0.763, 0.595, 2.13}, {0, 64, 64, 2.56, 0.854, 0.28, 0.0401, 0.914, 0.72, 2.36},
+    {0, 128, 48, 3.36, 0.542, 0.35, 0.0209, 0.799, 0.685, 2.03}, {0, 128, 64, 3.34, 0.804, 0.391, 0.0212, 0.702, 0.592, 2.28},
+    {1, 128, 64, 1.7, 1.95, 0.336, 0.0368, 0.161, 0, 0},        {1, 128, 128, 1.35, 3.62, 0.473, 0.054, 0.155, 0, 0},
+    {1, 128, 256, 1.73, 5.31, 0.753, 0.0213, 0.229, 0, 0},      {1, 192, 128, 0.443, 5.27, 0.6, 0.00571, 0.263, 0, 0},
+    {1, 192, 256, 0, 9.01, 0.891, 0.0228, 0.235, 0, 0},         {1, 256, 128, 0.96, 5.56, 0.698, 0.0136, 0.27, 0, 0},
+    {1, 256, 256, 0, 11.1, 1.13, 0.0183, 0.246, 0, 0}};
 template <typename T>
 void launch_i8(const I8Plan& p, const int8_t* a, const float* sa, int M, const int8_t* w, const float* sw, int N, int Kp, T* out,
                int* sums, hipStream_t st) {
@@ -500,25 +503,34 @@ void launch_i8(const I8Plan& p, const int8_t* a, const float* sa, int M, const i
   if (p.wide) {
 #define DLLMC_W(WM, WN, MI, NJ) \
   hipLaunchKernelGGL((k_i8_wide<T, WM, WN, MI, NJ>), grid, dim3(256), 0, st, a, sa, M, w, sw, N, Kp, out)
-    if (p.bm == 256) DLLMC_W(2, 2, 8, 8);
-    else DLLMC_W(2, 2, 4, 4);
+    switch (p.bm * 1000 + p.bn) {
+      case 256256: DLLMC_W(2, 2, 8, 8); break;
+      case 192256: DLLMC_W(2, 2, 6, 8); break;
+      case 256128: DLLMC_W(2, 2, 8, 4); break;
+      case 128256: DLLMC_W(2, 2, 4, 8); break;
+      case 192128: DLLMC_W(2, 2, 6, 4); break;
+      case 128128: DLLMC_W(2, 2, 4, 4); break;
+      default: DLLMC_W(2, 2, 4, 2); break;
+    }
 #undef DLLMC_W
     return;
   }
 #define DLLMC_R(RG, RB, NB) \
-  hipLaunchKernelGGL((k_i8_ring<T, RG, RB, NB, false>), grid, dim3(512), 0, st, a, sa, M, w, sw, N, Kp, p.per, out, sums)
-#define DLLMC_RN(RG, RB)              \
-  switch (p.bn / 16) {                \
-    case 1: DLLMC_R(RG, RB, 1); break; \
-    case 2: DLLMC_R(RG, RB, 2); break; \
-    case 3: DLLMC_R(RG, RB, 3); break; \
-    default: DLLMC_R(RG, RB, 4); break; \
+  hipLaunchKernelGGL((k_i8_ring<T, RG, RB, NB>), grid, dim3(512), 0, st, a, sa, M, w, sw, N, Kp, p.per, out, sums)
+  switch (p.bm * 100 + p.bn) {
+    case 1616: DLLMC_R(1, 1, 1); break;
+    case 1632: DLLMC_R(1, 1, 2); break;
+    case 1648: DLLMC_R(1, 1, 3); break;
+    case 1664: DLLMC_R(1, 1, 4); break;
+    case 3216: DLLMC_R(2, 1, 1); break;
+    case 3248: DLLMC_R(2, 1, 3); break;
+    case 3264: DLLMC_R(2, 1, 4); break;
+    case 6416: DLLMC_R(4, 1, 1); break;
+    case 6448: DLLMC_R(4, 1, 3); break;
+    case 6464: DLLMC_R(4, 1, 4); break;
+    case 12848: DLLMC_R(4, 2, 3); break;
+    default: DLLMC_R(4, 2, 4); break;
   }
-  if (p.bm == 16) { DLLMC_RN(1, 1) }
-  else if (p.bm == 32) { DLLMC_RN(2, 1) }
-  else if (p.bm == 64) { DLLMC_RN(4, 1) }
-  else { DLLMC_RN(4, 2) }
-#undef DLLMC_RN
 #undef DLLMC_R
   if (p.S > 1) {
     const long long g = (static_cast<long long>(M) * N + 255) / 256;
@@ -541,6 +553,27 @@ void quant8(const T* x, const int* rows, int M, int K, int8_t* q, float* scale, 
 }
 
 }  // namespace
+
+I8Plan plan_i8(int M, int N, int Kp) {
+  const int lines = Kp / 128;
+  const double mb_w = static_cast<double>(N) * Kp / 1e6, mn = static_cast<double>(M) * N / 1e6;
+  I8Plan best{};
+  double best_t = 1e300;
+  for (const I8Cost& c : kI8Costs) {
+    const long long mt = (M + c.bm - 1) / c.bm, nt = (N + c.bn - 1) / c.bn;
+    if (mt > 65535) continue;  // (the grid's second dimension)
+    for (int S = 1; S <= (c.wide ? 1 : 8); S *= 2) {
+      const int per = (lines + S - 1) / S, used = (lines + per - 1) / per;
+      const double rounds = static_cast<double>((mt * nt * used + 255) / 256);
+      const double t = c.start + rounds * (c.round + c.line * per) + mb_w * c.w + (used == 1 ? 2 * mn * c.out : used * 4 * mn * c.sums + c.add);
+      if (t < best_t) {
+        best_t = t;
+        best = {c.wide, c.bm, c.bn, used, per * 128};
+      }
+    }
+  }
+  return best;
+}
 
 void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
   if (dtype == 1) quant8(static_cast<const bf16_t*>(x), rows, M, K, q, scale, st);

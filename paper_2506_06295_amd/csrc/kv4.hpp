@@ -129,6 +129,8 @@ void launch_compact(int format, const int* rows, int M, int src_rows, int dst_ro
 // 8-bit rows of K rounded up to 128 bytes (kernels_i8.hip)
 inline size_t i8_row_bytes(int K) { return (static_cast<size_t>(K) + 127) / 128 * 128; }
 void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st);
+struct I8Plan { int wide, bm, bn, S, per; };  // wide: tile kernel; else ring of bm x bn and S slices of `per` bytes
+I8Plan plan_i8(int M, int N, int Kp);
 size_t linear_i8_scratch_bytes(int M, int N, int K);
 void launch_linear_i8(int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale, int N, int K,
                       void* out, void* scratch, hipStream_t st);
