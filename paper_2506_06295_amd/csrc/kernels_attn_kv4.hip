@@ -61,7 +61,8 @@ template <int D, bool PAGED> struct KeyLoader {
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const uint8_t* p = kc + static_cast<size_t>(krow[s]) * (D / 2) + lg * (D / 8);
+      // (a head's codes end below 2^24 * 128 bytes: a scalar base and a 32-bit offset)
+      const uint8_t* p = kc + (static_cast<uint32_t>(krow[s]) * (D / 2) + lg * (D / 8));
       if constexpr (D == 64) {
         const uint2 w = *reinterpret_cast<const uint2*>(p);
         b.k[s][0] = w.x; b.k[s][1] = w.y;
@@ -72,14 +73,14 @@ template <int D, bool PAGED> struct KeyLoader {
           b.k[s][4 * h] = w.x; b.k[s][4 * h + 1] = w.y; b.k[s][4 * h + 2] = w.z; b.k[s][4 * h + 3] = w.w;
         }
       }
-      const uint8_t* q = ks + static_cast<size_t>(krow[s]) * (D / 32);
-      b.ks[s] = D == 64 ? q[lg / 2] : D == 128 ? q[lg] : reinterpret_cast<const uint16_t*>(q)[lg];
+      const uint32_t q = static_cast<uint32_t>(krow[s]) * (D / 32);
+      b.ks[s] = D == 64 ? ks[q + lg / 2] : D == 128 ? ks[q + lg] : *reinterpret_cast<const uint16_t*>(ks + (q + 2 * lg));
     }
 #pragma unroll
     for (int t = 0; t < B::kV; ++t) {
       const int pc = (t * 64 + lane) % (D / 32);
-      b.v[t] = *reinterpret_cast<const uint4*>(vc + static_cast<size_t>(vrow[t]) * (D / 2) + pc * 16);
-      b.vs[t] = vs[static_cast<size_t>(vrow[t]) * (D / 32) + pc];
+      b.v[t] = *reinterpret_cast<const uint4*>(vc + (static_cast<uint32_t>(vrow[t]) * (D / 2) + pc * 16));
+      b.vs[t] = vs[static_cast<uint32_t>(vrow[t]) * (D / 32) + pc];
     }
   }
 };
@@ -345,13 +346,12 @@ template <typename T, int D, int QB, int NW, bool PAGED>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(few_waves(sizeof(T) == 4, D, QB)))) void k_attend_few(
     const T* __restrict__ q, AttendShape s, CacheView k, CacheView v, Keys keys, T* __restrict__ out, float* __restrict__ lse,
     float* __restrict__ part, float2* __restrict__ part_ml) {
-  // an item's ranges side by side, then the next row tile, which reads the same keys
+  // the row tiles of a head and range, which read the same keys, on one XCD
   AttendItem it;
-  int x = blockIdx.x;
-  it.range = s.KS > 1 ? x % s.KS : -1;
-  it.local = x / s.KS;
-  x = it.local;
+  int x = xcd_group_item(blockIdx.x, gridDim.x, s.tiles);
   it.tile = x % s.tiles; x /= s.tiles;
+  it.range = s.KS > 1 ? x % s.KS : -1; x /= s.KS;
+  it.local = x * s.tiles + it.tile;
   it.h = x % s.H_kv;
   it.b = x / s.H_kv;
   const size_t head = static_cast<size_t>(it.h) * k.cache_rows;
@@ -423,8 +423,8 @@ __device__ __forceinline__ void attend_tile_body(const bf16_t* __restrict__ q, c
 #pragma unroll
       for (int t = 0; t < kPieces; ++t) {
         const int row = PAGED ? __shfl(max(rk, 0), pkey[t], 64) : it.b * keys.n + min(blk * 64 + pkey[t], len - 1);
-        code[t] = *reinterpret_cast<const uint4*>(pc[t] + static_cast<size_t>(row) * (D / 2));
-        scale[t] = ps[t][static_cast<size_t>(row) * (D / 32)];
+        code[t] = *reinterpret_cast<const uint4*>(pc[t] + static_cast<uint32_t>(row) * (D / 2));
+        scale[t] = ps[t][static_cast<uint32_t>(row) * (D / 32)];
       }
     };
     auto expand = [&](int stage) {

@@ -5,8 +5,6 @@ namespace dllmc {
 
 namespace {
 
-constexpr int kEW = 16;  // wavefronts of the selection's workgroup
-
 // What positions are ordered by: 0 not there, then NaN, then the weights ascending (-0 as 0), then those always kept.
 __device__ __forceinline__ uint32_t keep_key(const float* acc, const Keys& keys, int b, int j, int len, int first, int last) {
   if (j >= len || keys.row(b, j) < 0) return 0;
@@ -17,19 +15,20 @@ __device__ __forceinline__ uint32_t keep_key(const float* acc, const Keys& keys,
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per sequence.  Wavefront w takes the positions [w P, (w + 1) P), P = 64 KPT, 64 neighbours at a time, so that
-// the order of positions is the order of (wavefront, trip, lane) and places come from ballots.  The k-th largest key by four
-// passes over its bytes; each pass counts the keys that agree with the bytes found so far in a histogram with a column per
-// lane (weights of one sequence share their exponents: in a single column most of a wavefront's adds would meet).
-// KPT > 0: keys in registers; 0: formed again in every pass.
-template <int KPT>
-__global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ acc, Keys keys, int keep, int first, int last,
-                                                    int* __restrict__ kept, int* __restrict__ kept_rows,
-                                                    int* __restrict__ new_lens, float* __restrict__ acc_out) {
-  __shared__ uint32_t hist[256 * 64];
-  __shared__ int bins[256], found[3], counts[2][kEW];
+// One workgroup of W wavefronts per sequence.  Wavefront w takes the positions [w P, (w + 1) P), P = 64 KPT, 64 neighbours at a time, so
+// that the order of positions is the order of (wavefront, trip, lane) and places come from ballots.  The k-th largest key by
+// up to four passes over its bytes, fewer where a pass ends between two bins; each counts the keys that agree with the bytes found so far in
+// a histogram with a column per lane (weights of one sequence share their exponents: in a single column most of a wavefront's
+// adds would meet).  KPT > 0: keys in registers; 0: formed again in every pass (beyond 32768 positions).
+template <int W, int KPT>
+__global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc, Keys keys, int keep, int first, int last,
+                                                  int* __restrict__ kept, int* __restrict__ kept_rows, int* __restrict__ new_lens,
+                                                  float* __restrict__ acc_out) {
+  constexpr int kThreads = 64 * W;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[256 * 64];
+  __shared__ int bins[256], found[3], counts[2][W];
   const int b = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int trips = KPT > 0 ? KPT : (keys.n + 64 * kEW - 1) / (64 * kEW);
+  const int trips = KPT > 0 ? KPT : (keys.n + kThreads - 1) / kThreads;
   const int len = keys.length(b), j0 = wave * trips * 64 + lane;
   uint32_t held[KPT > 0 ? KPT : 1];
   auto key = [&](int i) -> uint32_t {
@@ -44,16 +43,21 @@ __global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ ac
       for (int i = 0; i < trips; ++i) f(i);
     }
   };
+  auto clear = [&] {
+    for (int t = threadIdx.x; t < 256 * 16; t += kThreads) reinterpret_cast<uint4*>(hist)[t] = make_uint4(0, 0, 0, 0);
+  };
   if constexpr (KPT > 0) {
 #pragma unroll
     for (int i = 0; i < KPT; ++i) held[i] = keep_key(acc, keys, b, j0 + i * 64, len, first, last);
   }
+  clear();
   int mine = 0;
   each([&](int i) { mine += __popcll(__ballot(key(i) != 0)); });
   if (lane == 0) counts[0][wave] = mine;
   __syncthreads();
   int there = 0;
-  for (int w = 0; w < kEW; ++w) there += counts[0][w];
+#pragma unroll
+  for (int w = 0; w < W; ++w) there += counts[0][w];
   const int k = min(keep, there);
 
   // threshold: keys above it all stay, `quota` of those equal to it, the lowest positions
@@ -62,43 +66,54 @@ __global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ ac
   if (there > keep) {
     int want = k;  // of the keys that agree with the bytes found so far
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int t = threadIdx.x; t < 256 * 64; t += 64 * kEW) hist[t] = 0;
-      __syncthreads();
       each([&](int i) {
         const uint32_t u = key(i);
         if (u != 0 && (shift == 24 || (u >> (shift + 8)) == (threshold >> (shift + 8)))) atomicAdd(&hist[((u >> shift) & 255) * 64 + lane], 1u);
       });
       __syncthreads();
       {
-        const int bin = threadIdx.x / 4, part = threadIdx.x % 4;
+        constexpr int kParts = kThreads / 256;  // threads per bin
+        const int bin = threadIdx.x / kParts, part = threadIdx.x % kParts;
         int sum = 0;
-        for (int t = 0; t < 16; ++t) sum += hist[bin * 64 + part * 16 + (t + threadIdx.x) % 16];
-        sum += __shfl_xor(sum, 1, 64);
-        sum += __shfl_xor(sum, 2, 64);
+#pragma unroll
+        for (int t = 0; t < 16 / kParts; ++t) {  // (the 16 pieces of a bin start elsewhere in every bin: other banks)
+          const uint4 v = reinterpret_cast<const uint4*>(hist)[bin * 16 + (part + t * kParts + bin) % 16];
+          sum += v.x + v.y + v.z + v.w;
+        }
+        if (kParts >= 2) sum += __shfl_xor(sum, 1, 64);
+        if (kParts >= 4) sum += __shfl_xor(sum, 2, 64);
         if (part == 0) bins[bin] = sum;
       }
       __syncthreads();
       if (wave == 0) {
-        int c[4], above = 0;
-        for (int t = 0; t < 4; ++t) above += c[t] = bins[lane * 4 + t];
-        const int own = above;
+        const int4 v = reinterpret_cast<const int4*>(bins)[lane];
+        const int c[4] = {v.x, v.y, v.z, v.w};
+        const int own = c[0] + c[1] + c[2] + c[3];
+        int above = own;
         for (int o = 1; o < 64; o <<= 1) {
-          const int v = __shfl_down(above, o, 64);
-          if (lane + o < 64) above += v;
+          const int d = __shfl_down(above, o, 64);
+          if (lane + o < 64) above += d;
         }
         above -= own;  // keys in the bins of the lanes after this one
+#pragma unroll
         for (int t = 3; t >= 0; --t) {
           if (above < want && above + c[t] >= want) {
             found[0] = lane * 4 + t;
             found[1] = above;
+            found[2] = c[t];
           }
           above += c[t];
         }
       }
+      if (shift > 0) clear();  // (everybody has read its bins)
       __syncthreads();
       threshold |= static_cast<uint32_t>(found[0]) << shift;
       want -= found[1];
-      __syncthreads();
+      if (want == found[2]) {  // all of the bin: everything from its lowest key on
+        threshold -= threshold > 0 ? 1 : 0;
+        want = 0;
+        break;
+      }
     }
     quota = want;
   }
@@ -116,9 +131,10 @@ __global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ ac
   }
   __syncthreads();
   above = equal = 0;
-  for (int w = 0; w < wave; ++w) {
-    above += counts[0][w];
-    equal += counts[1][w];
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    above += w < wave ? counts[0][w] : 0;
+    equal += w < wave ? counts[1][w] : 0;
   }
   const size_t out0 = static_cast<size_t>(b) * keep;
   each([&](int i) {
@@ -136,7 +152,7 @@ __global__ __launch_bounds__(64 * kEW) void k_evict(const float* __restrict__ ac
     above += __popcll(hi);
     equal += __popcll(eq);
   });
-  for (int t = k + threadIdx.x; t < keep; t += 64 * kEW) {
+  for (int t = k + threadIdx.x; t < keep; t += kThreads) {
     kept[out0 + t] = -1;
     kept_rows[out0 + t] = -1;
     if (acc_out != nullptr) acc_out[out0 + t] = 0.f;
@@ -187,13 +203,16 @@ inline unsigned groups(long long items) {
 
 void launch_evict(const float* acc, int B, const Keys& keys, int keep, int first, int last, int* kept, int* kept_rows,
                   int* new_lens, float* acc_out, hipStream_t st) {
-#define DLLMC_E(KPT) \
-  hipLaunchKernelGGL(k_evict<KPT>, dim3(B), dim3(64 * kEW), 0, st, acc, keys, keep, first, last, kept, kept_rows, new_lens, acc_out)
+#define DLLMC_E(W, KPT) \
+  hipLaunchKernelGGL((k_evict<W, KPT>), dim3(B), dim3(64 * W), 0, st, acc, keys, keep, first, last, kept, kept_rows, new_lens, acc_out)
   const int n = keys.n;
-  if (n <= 1024) DLLMC_E(1);
-  else if (n <= 4096) DLLMC_E(4);
-  else if (n <= 16384) DLLMC_E(16);
-  else DLLMC_E(0);
+  if (n <= 256) DLLMC_E(4, 1);
+  else if (n <= 1024) DLLMC_E(4, 4);
+  else if (n <= 4096) DLLMC_E(16, 4);
+  else if (n <= 8192) DLLMC_E(16, 8);
+  else if (n <= 16384) DLLMC_E(16, 16);
+  else if (n <= 32768) DLLMC_E(16, 32);
+  else DLLMC_E(16, 0);
 #undef DLLMC_E
 }
 

@@ -1,9 +1,10 @@
 // Attention weight of every cached position: column sums of softmax(Q K^T / sqrt(d_h)) over queries and heads.
 //
-// A row's probabilities need its maximum and sum before any column can be added up, so scores are formed twice: k_weigh_stats
-// reduces every row over ranges of keys to (m, l), k_weigh_cols holds a block of keys in registers, walks the rows, and adds exp2(s -
-// m) / l per key; k_weigh_sum adds what heads and row shares left, in their order.  Where the caller has the rows'
-// log-sum-exp the first launch and its pass over the keys fall away.  No value is read and no probability leaves a register.
+// A row's probabilities need its maximum and sum before any column can be added up.  Up to 1024 keys k_weigh_short holds a head's
+// keys in the registers of one workgroup and forms every score once.  Beyond, scores are formed twice: k_weigh_stats reduces every row over
+// ranges of keys to (m, l), k_weigh_join those to z = m + log2 l, and k_weigh_cols holds a block of keys in registers, walks the rows and
+// adds exp2(s - z) per key; where the caller has the rows' log-sum-exp, the first two and their pass over the keys fall
+// away.  k_weigh_sum adds what heads and row shares left, in their order.  No value is read and no probability leaves a register.
 #include <type_traits>
 
 #include "kv4.hpp"
@@ -22,8 +23,9 @@ template <typename T, int D> struct KeyOperand<Kv4Tensor, T, D> {
   typedef bf16x8 Query[kC][kQ];
   static __device__ __forceinline__ int at(int lg, int c) { return lg * (D / 4) + 8 * c; }
   static __device__ __forceinline__ void load(const CacheView& v, int h, int row, int lg, Raw& r) {
-    const size_t i = static_cast<size_t>(h) * v.cache_rows + row;
-    const uint8_t* p = v.kv4.codes + i * (D / 2) + lg * (D / 8);
+    // (a head's codes end below 2^24 * 128 bytes: a scalar base and a 32-bit offset)
+    const size_t head = static_cast<size_t>(h) * v.cache_rows;
+    const uint8_t* p = v.kv4.codes + head * (D / 2) + (static_cast<uint32_t>(row) * (D / 2) + lg * (D / 8));
     if constexpr (D == 64) {
       const uint2 w = *reinterpret_cast<const uint2*>(p);
       r.w[0] = w.x; r.w[1] = w.y;
@@ -34,8 +36,9 @@ template <typename T, int D> struct KeyOperand<Kv4Tensor, T, D> {
         r.w[4 * t] = w.x; r.w[4 * t + 1] = w.y; r.w[4 * t + 2] = w.z; r.w[4 * t + 3] = w.w;
       }
     }
-    const uint8_t* q = v.kv4.scales + i * (D / 32);
-    r.s = D == 64 ? q[lg / 2] : D == 128 ? q[lg] : reinterpret_cast<const uint16_t*>(q)[lg];
+    const uint8_t* q = v.kv4.scales + head * (D / 32);
+    const uint32_t at = static_cast<uint32_t>(row) * (D / 32);
+    r.s = D == 64 ? q[at + lg / 2] : D == 128 ? q[at + lg] : *reinterpret_cast<const uint16_t*>(q + (at + 2 * lg));
   }
   static __device__ __forceinline__ void expand(const Raw& r, Frag& f) {
 #pragma unroll
@@ -45,12 +48,19 @@ template <typename T, int D> struct KeyOperand<Kv4Tensor, T, D> {
 #pragma unroll
     for (int c = 0; c < kC; ++c) load_query(row + at(lg, c), q[c]);
   }
+  template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      if constexpr (sizeof(T) == 2) q[c][0] = __builtin_bit_cast(bf16x8, piece(at(lg, c) / 8));
+      else split_query(piece(at(lg, c) / 4), piece(at(lg, c) / 4 + 1), q[c]);
+    }
+  }
   static __device__ __forceinline__ f32x4 scores(const Frag& k, const Query& q) {
-    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[0], q[0][kQ - 1], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
     for (int u = kQ - 1; u >= 0; --u)
 #pragma unroll
-      for (int c = 0; c < kC; ++c) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c], q[c][u], s, 0, 0, 0);
+      for (int c = u == kQ - 1 ? 1 : 0; c < kC; ++c) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c], q[c][u], s, 0, 0, 0);
     return s;
   }
 };
@@ -72,6 +82,10 @@ template <int D> struct KeyOperand<bf16_t, bf16_t, D> {
   static __device__ __forceinline__ void query(const bf16_t* row, int lg, Query& q) {
 #pragma unroll
     for (int c = 0; c < kC; ++c) q[c] = *reinterpret_cast<const bf16x8*>(row + at(lg, c));
+  }
+  template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(bf16x8, piece(at(lg, c) / 8));
   }
   static __device__ __forceinline__ f32x4 scores(const Frag& k, const Query& q) {
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -99,6 +113,10 @@ template <int D> struct KeyOperand<float, float, D> {
 #pragma unroll
     for (int c = 0; c < kC; ++c) q[c] = *reinterpret_cast<const f32x4*>(row + at(lg, c));
   }
+  template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(f32x4, piece(at(lg, c) / 4));
+  }
   static __device__ __forceinline__ f32x4 scores(const Frag& k, const Query& q) {
     f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;  // (two chains: an instruction may not wait for its predecessor)
 #pragma unroll
@@ -115,22 +133,26 @@ template <int D> struct KeyOperand<float, float, D> {
 struct WeighShape {
   int Mq, H_q, H_kv, G, NR;  // NR = Mq * G rows of a KV head
   int tiles, KS, per;        // stats: tiles of 16 QB rows, key ranges, 32-key blocks per range
-  int blocks, RS, share;     // columns: workgroups of 64 KB keys per head, row shares, 16-row tiles per share
+  int blocks, RS, share;     // columns: workgroups of 64 KB keys per head, row shares, 16-row tiles (stages, see there) per share
 };
 __device__ __forceinline__ size_t row_of(const WeighShape& s, int b, int h, int r) {
   const int i = s.G == 1 ? r : r / s.G;
   return (static_cast<size_t>(b) * s.Mq + i) * s.H_q + h * s.G + (r - i * s.G);
 }
 
-// (m, l) of 16 QB rows over a range of keys, base 2; the wavefronts deal the range's blocks of 32 keys, the next one in flight.
+// (m, l) of 16 QB rows over a range of keys, base 2, or z where the range is all of them; the eight wavefronts deal the range's blocks
+// of 32 keys, the next one in flight.  Bound by vector instructions (one per 5 cycles: 4.5 a score) and the products
+// beside them: 0.66 of what the products alone would take, 4608 rows x 4608 keys x 32 heads.
+constexpr int kSW = 8;
 template <typename F, typename T, int D, int QB>
-__global__ __launch_bounds__(256, D == 256 ? (sizeof(T) == 4 ? 1 : 2) : QB == 1 && sizeof(T) == 2 ? 3 : 2) void k_weigh_stats(const T* __restrict__ q, WeighShape s, CacheView k, Keys keys,
-                                                                     float2* __restrict__ ml) {
+__global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_stats(const T* __restrict__ q, WeighShape s, CacheView k,
+                                                                                            Keys keys, float2* __restrict__ ml,
+                                                                                            float* __restrict__ z) {
   typedef KeyOperand<F, T, D> Op;
-  __shared__ float2 hand[4][16 * QB];
+  __shared__ float2 hand[kSW][16 * QB];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
-  int x = blockIdx.x;
+  int x = xcd_group_item(blockIdx.x, gridDim.x, s.tiles);  // tiles of one head and range read the same keys
   const int tile = x % s.tiles; x /= s.tiles;
   const int range = x % s.KS; x /= s.KS;
   const int h = x % s.H_kv, b = x / s.H_kv;
@@ -198,15 +220,15 @@ __global__ __launch_bounds__(256, D == 256 ? (sizeof(T) == 4 ? 1 : 2) : QB == 1 
     int r[2];
     rows_of(blk, r);
     fetch(r, b0);
-    rows_of(min(blk + 4, blk1 - 1), r);
+    rows_of(min(blk + kSW, blk1 - 1), r);
 #pragma unroll
     for (int i = 0; i < QB; ++i) Op::query(q + row_of(s, b, h, min(r0 + i * 16 + ln, s.NR - 1)) * D, lg, qf[i]);
-    for (; blk + 4 < blk1; blk += 8) {
+    for (; blk + kSW < blk1; blk += 2 * kSW) {
       fetch(r, b1);
-      rows_of(min(blk + 8, blk1 - 1), r);
+      rows_of(min(blk + 2 * kSW, blk1 - 1), r);
       use(b0);
       fetch(r, b0);
-      rows_of(min(blk + 12, blk1 - 1), r);
+      rows_of(min(blk + 3 * kSW, blk1 - 1), r);
       use(b1);
     }
     if (blk < blk1) use(b0);
@@ -227,111 +249,212 @@ __global__ __launch_bounds__(256, D == 256 ? (sizeof(T) == 4 ? 1 : 2) : QB == 1 
   if (threadIdx.x < 16 * QB && r0 + static_cast<int>(threadIdx.x) < s.NR) {
     float2 v = hand[0][threadIdx.x];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) v = join(v, hand[w][threadIdx.x]);
-    ml[row_of(s, b, h, r0 + threadIdx.x) * s.KS + range] = v;
+    for (int w = 1; w < kSW; ++w) v = join(v, hand[w][threadIdx.x]);
+    const size_t w = row_of(s, b, h, r0 + threadIdx.x);
+    if (s.KS == 1) z[w] = v.x + log2f(v.y);
+    else ml[w * s.KS + range] = v;
   }
 }
 
-// Column sums: a wavefront holds 16 KB keys of one KV head and walks its share of the head's rows, 16 at a time, the next 16 in
-// flight.  part[(share * B + b) * H_kv + h][n].
+// z = m + log2 l over the ranges, one thread per row
+__global__ __launch_bounds__(256) void k_weigh_join(const float2* __restrict__ ml, int KS, int rows, float* __restrict__ z) {
+  const int w = blockIdx.x * 256 + threadIdx.x;
+  if (w >= rows) return;
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i < KS; ++i) {
+    const float2 c = ml[static_cast<size_t>(w) * KS + i];
+    const float M = fmaxf(m, c.x), u = M == -INFINITY ? 0.f : M;
+    l = (l != l ? l : l * __builtin_amdgcn_exp2f(m - u)) + (c.y != c.y ? c.y : c.y * __builtin_amdgcn_exp2f(c.x - u));
+    m = M;
+  }
+  z[w] = m + log2f(l);
+}
+
+// 16 KB column sums of a wavefront leave for part[j], zero where there is no key; `there`: keys of each 16
+template <int KB>
+__device__ __forceinline__ void store_columns(f32x4 (&sum)[KB], const uint32_t (&there)[KB], int key0, int n, int ln, int lg, float* out) {
+#pragma unroll
+  for (int t = 0; t < KB; ++t) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[t][e] = row16_sum(sum[t][e]);
+    // lane ln < 4 of each 16 takes key 4 lg + ln
+    const float v = ln == 0 ? sum[t][0] : ln == 1 ? sum[t][1] : ln == 2 ? sum[t][2] : sum[t][3];
+    const int j = key0 + t * 16 + 4 * lg + ln;
+    if (ln < 4 && j < n) out[j] = (there[t] >> (4 * lg + ln)) & 1 ? v : 0.f;
+  }
+}
+template <typename Op, int KB>
+__device__ __forceinline__ void load_keys(const CacheView& k, const Keys& keys, int b, int h, int key0, int len, int ln, int lg,
+                                          typename Op::Frag (&f)[KB], uint32_t (&there)[KB]) {
+  int r[KB];
+  typename Op::Raw raw[KB];
+#pragma unroll
+  for (int t = 0; t < KB; ++t) r[t] = key0 + t * 16 + ln < len ? keys.row(b, key0 + t * 16 + ln) : -1;
+#pragma unroll
+  for (int t = 0; t < KB; ++t) {
+    there[t] = static_cast<uint32_t>(__ballot(r[t] >= 0));  // (lanes 0 .. 15: the keys)
+    Op::load(k, h, max(r[t], 0), lg, raw[t]);  // what is not there: row 0, counts for nothing
+  }
+#pragma unroll
+  for (int t = 0; t < KB; ++t) Op::expand(raw[t], f[t]);
+}
+
+// Column sums: a wavefront holds 16 KB keys of one KV head and walks its share of the head's rows; rows come in stages of 8 KB (16
+// rows at least) through a ring in LDS that the four wavefronts share, with their z.  part[(share * B + b) * H_kv + h][n].
+// With every wavefront fetching its rows by itself, 16 ahead, a launch of 512 rows x 4608 keys x 32 heads waited on trips to the L2: 60 us.
+template <typename T, int D> struct WeighStage {
+  static constexpr int kRow = D * static_cast<int>(sizeof(T)), kRows = kRow >= 512 ? 16 : 8192 / kRow;
+  static constexpr int kVecs = kRows * kRow / 16, kLoads = kVecs / 256, kStages = 4;
+};
 template <typename F, typename T, int D, int KB>
-__global__ __launch_bounds__(256, D == 256 && sizeof(T) == 4 ? 1 : 2) void k_weigh_cols(const T* __restrict__ q, WeighShape s, CacheView k, Keys keys,
-                                                       const float* __restrict__ lse, const float2* __restrict__ ml,
-                                                       float* __restrict__ part) {
+__device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const WeighShape& s, const CacheView& k, const Keys& keys,
+                                                const float* __restrict__ z, float zmul, float* __restrict__ part) {
   typedef KeyOperand<F, T, D> Op;
+  typedef WeighStage<T, D> St;
+  constexpr int NS = St::kStages, kChunks = St::kRow / 16, kMix = kChunks < 16 ? kChunks : 16;
+  __shared__ __attribute__((aligned(1024))) uint4 lds[NS * St::kVecs + NS * 4 * 16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
-  int x = blockIdx.x;
+  int x = xcd_group_item(blockIdx.x, gridDim.x, s.blocks);  // key blocks of one head and share read the same rows
   const int blk = x % s.blocks; x /= s.blocks;
   const int share = x % s.RS; x /= s.RS;
   const int h = x % s.H_kv, b = x / s.H_kv;
   const int key0 = (blk * 4 + wave) * 16 * KB, len = keys.length(b);
   const int B = gridDim.x / (s.blocks * s.RS * s.H_kv);
-  if (key0 >= keys.n) return;
   float* out = part + (static_cast<size_t>(share * B + b) * s.H_kv + h) * keys.n;
+  const int t0 = share * s.share, t1 = min((s.NR + St::kRows - 1) / St::kRows, t0 + s.share);
+
+  // loader: instruction j of a stage copies 1 KB, wavefront w issues kLoads w .. + kLoads - 1 and its own copy of z
+  auto issue = [&](int slot, int t) {
+#pragma unroll
+    for (int j = 0; j < St::kLoads; ++j) {
+      const int v = (wave * St::kLoads + j) * 64 + lane, r = v / kChunks, c = (v % kChunks) ^ (r % kMix);
+      const size_t w = row_of(s, b, h, min(t * St::kRows + r, s.NR - 1));
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(q + w * D) + c, &lds[slot * St::kVecs + (wave * St::kLoads + j) * 64],
+                                       16, 0, 0);
+    }
+    const size_t w = row_of(s, b, h, min(t * St::kRows + lane % St::kRows, s.NR - 1));
+    __builtin_amdgcn_global_load_lds(z + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 16], 4, 0, 0);
+  };
+#pragma unroll
+  for (int t = 0; t < NS - 1; ++t)
+    if (t0 + t < t1) issue(t, t0 + t);
   f32x4 sum[KB];
+  uint32_t there[KB];
+  typename Op::Frag kf[KB];
 #pragma unroll
   for (int t = 0; t < KB; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load_keys<Op, KB>(k, keys, b, h, key0, len, ln, lg, kf, there);
+  const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
+  int slot = 0;
+  for (int t = t0; t < t1; ++t) {
+    const int rem = t1 - 1 - t;
+    if (rem >= NS - 2) wait_vmcnt_lds<(NS - 2) * (St::kLoads + 1)>();
+    else if (rem == 1) wait_vmcnt_lds<St::kLoads + 1>();
+    else wait_vmcnt_lds<0>();
+    __builtin_amdgcn_s_barrier();  // stage t is there for everybody, and everybody has read stage t - 1, which is filled next
+    if (t + NS - 1 < t1) issue(slot == 0 ? NS - 1 : slot - 1, t + NS - 1);
+    if (key0 < len) {
+#pragma unroll
+      for (int g = 0; g < St::kRows / 16; ++g) {
+        const int r = g * 16 + ln;
+        float zr = reinterpret_cast<const float*>(&lds[NS * St::kVecs + (slot * 4 + wave) * 16])[r] * zmul;
+        if (t * St::kRows + r >= s.NR) zr = INFINITY;  // rows past the last one weigh nothing
+        typename Op::Query qf;
+        Op::query_pieces([&](int c) { return lds[slot * St::kVecs + r * kChunks + (c ^ (r % kMix))]; }, lg, qf);
+#pragma unroll
+        for (int u = 0; u < KB; ++u) {
+          const f32x4 st = Op::scores(kf[u], qf);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[u][e] += __builtin_amdgcn_exp2f(fmaf(st[e], sl2e, -zr));
+        }
+      }
+    }
+    slot = slot + 1 < NS ? slot + 1 : 0;
+  }
+  if (key0 < keys.n) store_columns<KB>(sum, there, key0, keys.n, ln, lg, out);
+}
+template <typename F, typename T, int D, int KB>
+__global__ __launch_bounds__(256, D == 256 && sizeof(T) == 4 ? 1 : 2) void k_weigh_cols(const T* __restrict__ q, WeighShape s, CacheView k,
+                                                                                 Keys keys, const float* __restrict__ z, float zmul,
+                                                                                 float* __restrict__ part) {
+  weigh_cols_body<F, T, D, KB>(q, s, k, keys, z, zmul, part);
+}
+
+// Up to 128 KB keys: the eight wavefronts of a workgroup hold them all, 16 KB each, and walk a share of the head's rows 16 at a time.
+// Scores stay in registers while the wavefronts exchange their maxima and sums; no second pass, no z.
+template <typename F, typename T, int D, int KB>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_short(const T* __restrict__ q, WeighShape s, CacheView k,
+                                                                                         Keys keys, float* __restrict__ part) {
+  typedef KeyOperand<F, T, D> Op;
+  __shared__ float2 ml[2][8][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int ln = lane % 16, lg = lane / 16;
+  int x = xcd_group_item(blockIdx.x, gridDim.x, s.RS);  // shares of one head read the same keys
+  const int share = x % s.RS; x /= s.RS;
+  const int h = x % s.H_kv, b = x / s.H_kv;
+  const int key0 = wave * 16 * KB, len = keys.length(b);
+  const int B = gridDim.x / (s.RS * s.H_kv);
+  f32x4 sum[KB];
   uint32_t there[KB];
-  if (key0 < len) {
-    typename Op::Frag kf[KB];
-    {
-      int r[KB];
-      typename Op::Raw raw[KB];
+  typename Op::Frag kf[KB];
+  typename Op::Query qf;
+  const int t0 = share * s.share, t1 = min((s.NR + 15) / 16, t0 + s.share);
+  auto fetch = [&](int t) { Op::query(q + row_of(s, b, h, min(t * 16 + ln, s.NR - 1)) * D, lg, qf); };
+  fetch(t0);
 #pragma unroll
-      for (int t = 0; t < KB; ++t) r[t] = key0 + t * 16 + ln < len ? keys.row(b, key0 + t * 16 + ln) : -1;
+  for (int t = 0; t < KB; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load_keys<Op, KB>(k, keys, b, h, key0, len, ln, lg, kf, there);
+  uint32_t mine = 0;  // bit 4 t + e: this lane's key e of the 16 t-th is there
 #pragma unroll
-      for (int t = 0; t < KB; ++t) {
-        there[t] = static_cast<uint32_t>(__ballot(r[t] >= 0));
-        Op::load(k, h, max(r[t], 0), lg, raw[t]);
+  for (int t = 0; t < KB; ++t) mine |= ((there[t] >> (4 * lg)) & 15u) << (4 * t);
+  const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
+  for (int t = t0; t < t1; ++t) {
+    f32x4 st[KB];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int u = 0; u < KB; ++u) st[u] = Op::scores(kf[u], qf);
+    if (t + 1 < t1) fetch(t + 1);
+#pragma unroll
+    for (int u = 0; u < KB; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        st[u][e] = (mine >> (4 * u + e)) & 1 ? st[u][e] * sl2e : -INFINITY;
+        m = fmaxf(m, st[u][e]);
       }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int t = 0; t < KB; ++t) Op::expand(raw[t], kf[t]);
+    for (int u = 0; u < KB; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        st[u][e] = __builtin_amdgcn_exp2f(st[u][e] - ref);
+        l += st[u][e];
+      }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (lg == 0) ml[t & 1][wave][ln] = make_float2(m, l);
+    __syncthreads();
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) M = fmaxf(M, ml[t & 1][w][ln].x);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {  // (a sum may be NaN beside a maximum of minus infinity)
+      const float2 c = ml[t & 1][w][ln];
+      L += c.y != c.y ? c.y : c.x == -INFINITY ? 0.f : c.y * __builtin_amdgcn_exp2f(c.x - M);
     }
-    const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
-    const int t1 = min((s.NR + 15) / 16, (share + 1) * s.share);
-    struct Rows { typename Op::Query q; float z; };
-    auto fetch = [&](int t, Rows& v) {
-      const int r = t * 16 + ln;
-      const size_t w = row_of(s, b, h, min(r, s.NR - 1));
-      Op::query(q + w * D, lg, v.q);
-      if (lse != nullptr) {
-        v.z = lse[w] * kLog2e;
-      } else {  // the ranges' (m, l), a quarter of them per group of lanes
-        float m = -INFINITY, l = 0.f;
-        for (int i = lg; i < s.KS; i += 4) {
-          const float2 c = ml[w * s.KS + i];
-          const float M = fmaxf(m, c.x), u = M == -INFINITY ? 0.f : M;
-          l = l * __builtin_amdgcn_exp2f(m - u) + (c.y != c.y ? c.y : c.y * __builtin_amdgcn_exp2f(c.x - u));
-          m = M;
-        }
+    // what this wavefront's exponentials are short of; nothing for rows past the last one and wavefronts without keys
+    float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;
+    if (L != L) f = L;
+    if (t * 16 + ln >= s.NR) f = 0.f;
 #pragma unroll
-        for (int o = 16; o < 64; o <<= 1) {
-          const float m2 = __shfl_xor(m, o, 64), l2 = __shfl_xor(l, o, 64), M = fmaxf(m, m2), u = M == -INFINITY ? 0.f : M;
-          const float f1 = __builtin_amdgcn_exp2f(m - u), f2 = __builtin_amdgcn_exp2f(m2 - u);
-          l = (l != l ? l : l * f1) + (l2 != l2 ? l2 : l2 * f2);
-          m = M;
-        }
-        v.z = m + __builtin_amdgcn_logf(l);  // (base 2)
-      }
-      if (r >= s.NR) v.z = INFINITY;  // rows past the last one weigh nothing
-    };
-    auto use = [&](const Rows& v) {
+    for (int u = 0; u < KB; ++u)
 #pragma unroll
-      for (int t = 0; t < KB; ++t) {
-        const f32x4 st = Op::scores(kf[t], v.q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[t][e] += __builtin_amdgcn_exp2f(fmaf(st[e], sl2e, -v.z));
-      }
-    };
-    int t = share * s.share;
-    if (t < t1) {
-      Rows v0, v1;
-      fetch(t, v0);
-      for (; t + 1 < t1; t += 2) {
-        fetch(t + 1, v1);
-        use(v0);
-        fetch(min(t + 2, t1 - 1), v0);
-        use(v1);
-      }
-      if (t < t1) use(v0);
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < KB; ++t) there[t] = 0;
+      for (int e = 0; e < 4; ++e) sum[u][e] += (t * 16 + ln >= s.NR) ? 0.f : st[u][e] * f;
   }
-#pragma unroll
-  for (int t = 0; t < KB; ++t) {
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[t][e] += __shfl_xor(sum[t][e], o, 64);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = key0 + t * 16 + 4 * lg + e;
-      if (ln == 0 && j < keys.n) out[j] = (there[t] >> (4 * lg + e)) & 1 ? sum[t][e] : 0.f;
-    }
-  }
+  if (key0 < keys.n)
+    store_columns<KB>(sum, there, key0, keys.n, ln, lg, part + (static_cast<size_t>(share * B + b) * s.H_kv + h) * keys.n);
 }
 
 // acc_out[b][j] = acc_in[b][j] + the parts of all shares and heads, 16 wavefronts that take every 16th of them
@@ -353,64 +476,103 @@ __global__ __launch_bounds__(1024) void k_weigh_sum(const float* __restrict__ pa
   acc_out[at] = (acc_in != nullptr ? acc_in[at] : 0.f) + sum;
 }
 
-struct WeighPlan { int QB, KB; WeighShape s; };
+// most 16s of keys a wavefront's registers hold: fragments of at most 128 of them
+constexpr int short_blocks(bool f32_keys, bool f32, int D) { return (f32_keys ? 512 : f32 ? 512 : 1024) / D < 8 ? (f32_keys ? 512 : f32 ? 512 : 1024) / D : 8; }
+
+struct WeighPlan { int QB, KB; bool brief; WeighShape s; };
 WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
   WeighPlan p{};
   WeighShape& s = p.s;
   s.Mq = Mq; s.H_q = H_q; s.H_kv = H_kv; s.G = H_q / H_kv; s.NR = Mq * s.G;
+  const long long heads = static_cast<long long>(B) * H_kv;
+  const int most = short_blocks(format == 0, dtype == 0, d_h);
+  if (n <= 128 * most) {
+    p.brief = true;
+    p.KB = n <= 256 || most == 2 ? 2 : n <= 512 || most == 4 ? 4 : 8;
+    const int rt = (s.NR + 15) / 16;
+    long long RS = heads >= 128 ? 1 : 128 / heads;
+    if (RS > rt) RS = rt;
+    s.share = static_cast<int>((rt + RS - 1) / RS);
+    s.RS = (rt + s.share - 1) / s.share;
+    return p;
+  }
   p.QB = s.NR <= 16 || dtype == 0 || d_h == 256 ? 1 : s.NR <= 32 ? 2 : 4;
   s.tiles = (s.NR + 16 * p.QB - 1) / (16 * p.QB);
   const int nblk = (n + 31) / 32;
-  const long long items = static_cast<long long>(B) * H_kv * s.tiles;
-  long long KS = items >= 512 ? 1 : 512 / items;
-  const int most = (nblk + 7) / 8;
-  KS = KS > most ? most : KS;
+  const long long items = heads * s.tiles;
+  long long KS = items >= 256 ? 1 : 256 / items;
+  const int split = (nblk + 2 * kSW - 1) / (2 * kSW);  // two blocks a wavefront at least
+  KS = KS > split ? split : KS;
   KS = KS > 64 ? 64 : KS < 1 ? 1 : KS;
   s.per = static_cast<int>((nblk + KS - 1) / KS);
   s.KS = (nblk + s.per - 1) / s.per;
   p.KB = (format == 0 || d_h == 256) ? 2 : 4;
   s.blocks = (n + 64 * p.KB - 1) / (64 * p.KB);
-  const int rt = (s.NR + 15) / 16;
-  const long long groups = static_cast<long long>(B) * H_kv * s.blocks;
-  long long RS = groups >= 512 ? 1 : 512 / groups;
-  if (RS > rt) RS = rt;
-  s.share = static_cast<int>((rt + RS - 1) / RS);
-  s.RS = (rt + s.share - 1) / s.share;
+  const int row = d_h * (dtype == 1 ? 2 : 4), stage = row >= 512 ? 16 : 8192 / row, st = (s.NR + stage - 1) / stage;
+  const long long groups = heads * s.blocks;
+  double best = 1e300;
+  for (int RS = 1; RS <= 16 && RS <= st; ++RS) {
+    const int share = (st + RS - 1) / RS, used = (st + share - 1) / share;
+    const double t = static_cast<double>((groups * used + 511) / 512) * (3 + share) + 0.1 * used;
+    if (t < best) {
+      best = t;
+      s.share = share;
+      s.RS = used;
+    }
+  }
   return p;
 }
 
 }  // namespace
 
 size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
-  const WeighShape s = plan_weigh(dtype, format, B, Mq, n, H_q, H_kv, d_h).s;
-  return static_cast<size_t>(B) * Mq * H_q * s.KS * sizeof(float2) + static_cast<size_t>(s.RS) * B * H_kv * n * sizeof(float);
+  const WeighPlan p = plan_weigh(dtype, format, B, Mq, n, H_q, H_kv, d_h);
+  const size_t rows = static_cast<size_t>(B) * Mq * H_q;
+  return (p.brief ? 0 : (rows * (2 * p.s.KS + 1) + 1) / 2 * 2 * sizeof(float)) + static_cast<size_t>(p.s.RS) * B * H_kv * n * sizeof(float);
 }
 
-void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
-                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
-                              hipStream_t st) {
-  const WeighPlan p = plan_weigh(dtype, format, B, Mq, keys.n, H_q, H_kv, d_h);
+namespace {
+void launch_weigh(const WeighPlan& p, int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
+                  int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch, hipStream_t st) {
   const WeighShape& s = p.s;
+  const size_t count = static_cast<size_t>(B) * Mq * H_q;
   float2* ml = static_cast<float2*>(scratch);
-  float* part = reinterpret_cast<float*>(ml + static_cast<size_t>(B) * Mq * H_q * s.KS);
-  const dim3 rows(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.tiles * s.KS));
-  const dim3 cols(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.blocks * s.RS));
+  float* z = static_cast<float*>(scratch) + 2 * s.KS * count;
+  float* part = static_cast<float*>(scratch) + (p.brief ? 0 : (count * (2 * s.KS + 1) + 1) / 2 * 2);
   auto go = [&](auto f, auto t, auto d) {
     typedef decltype(f) F;
     typedef decltype(t) T;
     constexpr int D = decltype(d)::value;
+    constexpr bool f32_keys = std::is_same<F, float>::value, f32 = sizeof(T) == 4;
     const T* qt = static_cast<const T*>(q);
-    if (lse == nullptr) {
-      if constexpr (sizeof(T) == 4 || D == 256) {
-        hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(256), 0, st, qt, s, k, keys, ml);
-      } else {
-        if (p.QB == 1) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(256), 0, st, qt, s, k, keys, ml);
-        else if (p.QB == 2) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 2>), rows, dim3(256), 0, st, qt, s, k, keys, ml);
-        else hipLaunchKernelGGL((k_weigh_stats<F, T, D, 4>), rows, dim3(256), 0, st, qt, s, k, keys, ml);
+    if (p.brief) {
+      const dim3 grid(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.RS));
+      constexpr int most = short_blocks(f32_keys, f32, D);
+      if (p.KB == 2) hipLaunchKernelGGL((k_weigh_short<F, T, D, 2>), grid, dim3(512), 0, st, qt, s, k, keys, part);
+      if constexpr (most >= 4) {
+        if (p.KB == 4) hipLaunchKernelGGL((k_weigh_short<F, T, D, 4>), grid, dim3(512), 0, st, qt, s, k, keys, part);
       }
+      if constexpr (most >= 8) {
+        if (p.KB == 8) hipLaunchKernelGGL((k_weigh_short<F, T, D, 8>), grid, dim3(512), 0, st, qt, s, k, keys, part);
+      }
+      return;
     }
-    constexpr int KB = std::is_same<F, float>::value || D == 256 ? 2 : 4;
-    hipLaunchKernelGGL((k_weigh_cols<F, T, D, KB>), cols, dim3(256), 0, st, qt, s, k, keys, lse, ml, part);
+    if (lse == nullptr) {
+      const dim3 rows(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.tiles * s.KS));
+      if constexpr (f32 || D == 256) {
+        hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+      } else {
+        if (p.QB == 1) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+        else if (p.QB == 2) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 2>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+        else hipLaunchKernelGGL((k_weigh_stats<F, T, D, 4>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+      }
+      if (s.KS > 1)
+        hipLaunchKernelGGL(k_weigh_join, dim3(static_cast<unsigned>((count + 255) / 256)), dim3(256), 0, st, ml, s.KS, static_cast<int>(count),
+                         z);
+    }
+    constexpr int KB = f32_keys || D == 256 ? 2 : 4;
+    hipLaunchKernelGGL((k_weigh_cols<F, T, D, KB>), dim3(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.blocks * s.RS)),
+                       dim3(256), 0, st, qt, s, k, keys, lse ? lse : z, lse ? kLog2e : 1.f, part);
   };
   auto with_d = [&](auto f, auto t) {
     if (d_h == 64) go(f, t, std::integral_constant<int, 64>{});
@@ -427,6 +589,15 @@ void launch_attention_weights(int dtype, int format, const void* q, int B, int M
   }
   hipLaunchKernelGGL(k_weigh_sum, dim3(static_cast<unsigned>(B * ((keys.n + 63) / 64))), dim3(1024), 0, st, part, s.RS, B, H_kv, keys.n,
                      acc_in, acc_out);
+}
+
+}  // namespace
+
+void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
+                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
+                              hipStream_t st) {
+  launch_weigh(plan_weigh(dtype, format, B, Mq, keys.n, H_q, H_kv, d_h), dtype, format, q, B, Mq, k, keys, H_q, H_kv, d_h, lse, acc_in,
+               acc_out, scratch, st);
 }
 
 }  // namespace dllmc

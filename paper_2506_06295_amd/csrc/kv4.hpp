@@ -41,6 +41,24 @@ struct Keys {
   }
 };
 
+// Workgroups are handed to the 8 XCDs round-robin and each XCD has its own L2: the i-th of `all` workgroups takes the item below, such
+// that the `group` items that follow each other and read the same memory run on one XCD.  A bijection for any `all`, a multiple of
+// `group`; groups beyond the last multiple of 8 go as they come.
+__device__ __forceinline__ int xcd_group_item(int i, int all, int group) {
+  const int n8 = all / group & ~7;
+  if (group == 1 || i >= n8 * group) return i;
+  const int idx = i >> 3;
+  return (idx / group * 8 + (i & 7)) * group + idx % group;
+}
+
+// sum over the 16 lanes of a row of lanes, in all of them
+__device__ __forceinline__ float row16_sum(float v) {
+  v += dpp_xor1(v);
+  v += dpp_xor2(v);
+  v += dpp_half_mirror(v);
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false));  // (lane 15 - l of the 16)
+}
+
 // Scale byte of a block whose largest magnitude has the bits `top`: 127 + the smallest e with top <= 6 * 2^e = 1.5 * 2^(e + 2), so
 // that nothing saturates; at least 2 (no value below 2^-126), at most 252 (6 * 2^125 is finite: above it values do saturate).
 __device__ __forceinline__ uint32_t kv4_scale_byte(uint32_t top) {
@@ -90,9 +108,9 @@ template <> struct Parts<float> { static constexpr int kQ = 3, kP = 3; };
 __device__ __forceinline__ void load_query(const bf16_t* p, bf16x8 (&f)[1]) {
   f[0] = *reinterpret_cast<const bf16x8*>(p);
 }
-__device__ __forceinline__ void load_query(const float* p, bf16x8 (&f)[3]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+__device__ __forceinline__ void split_query(const uint4& lo, const uint4& hi, bf16x8 (&f)[3]) {
+  float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
 #pragma unroll
   for (int u = 0; u < 3; ++u) {
     uint32_t w[4];
@@ -104,6 +122,9 @@ __device__ __forceinline__ void load_query(const float* p, bf16x8 (&f)[3]) {
     }
     f[u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
   }
+}
+__device__ __forceinline__ void load_query(const float* p, bf16x8 (&f)[3]) {
+  split_query(reinterpret_cast<const uint4*>(p)[0], reinterpret_cast<const uint4*>(p)[1], f);
 }
 
 void launch_kv4_store(int dtype, const void* x, int M, int width, const int* rows, Kv4Tensor c, int cache_rows, int d_h,
