@@ -326,6 +326,15 @@ int32_t dllmc_plan_vverify(int32_t dtype, int32_t rows, int32_t d, int32_t d_kv)
  * d_q, heads of 128, 3: V-verify of N = d_kv columns.  *cols (may be NULL): the tile's columns (gate/up: of each matrix). */
 int32_t dllmc_plan_tile(int32_t launch, int32_t M, int32_t N, int32_t N0, int32_t K, int32_t* cols);
 
+/* Host-only: the number of key ranges into which dllmc_op_attention_kv4 cuts its work; *rows (may be NULL) rows of a workgroup (a
+ * KV head's Mq * H_q / H_kv rows are dealt in tiles of that many), *waves its wavefronts, *whole tiles that are not cut. */
+int32_t dllmc_plan_attention_kv4(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv, int32_t d_h,
+                                 int32_t* rows, int32_t* waves, int32_t* whole);
+/* Host-only: keys that dllmc_op_attention_weights holds per wavefront; *ranges (may be NULL) key ranges of the launch that sums rows,
+ * 0 where one launch does both, *row_blocks rows of its workgroups, *shares into how many shares a head's rows are dealt. */
+int32_t dllmc_plan_attention_weights(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n, int32_t H_q,
+                                     int32_t H_kv, int32_t d_h, int32_t* ranges, int32_t* row_blocks, int32_t* shares);
+
 /* Host-only: rows of the tiles that dllmc_op_linear_i8 takes; *cols (may be NULL) their columns, *slices the slices of the contraction
  * (more than one: a launch adds them), *whole 1: the contraction of a tile is walked by wavefronts of a quarter of the tile each, 0:
  * wavefronts share it. */

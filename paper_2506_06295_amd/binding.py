@@ -36,7 +36,7 @@ EXPORTS = (
     "dllmc_kv4_bytes", "dllmc_op_kv4_store", "dllmc_op_kv4_load", "dllmc_op_attention_kv4_scratch_bytes",
     "dllmc_op_attention_kv4", "dllmc_op_attention_weights_scratch_bytes", "dllmc_op_attention_weights", "dllmc_op_evict",
     "dllmc_op_compact", "dllmc_i8_row_bytes", "dllmc_op_quant8", "dllmc_op_linear_i8_scratch_bytes", "dllmc_op_linear_i8",
-    "dllmc_plan_linear_i8",
+    "dllmc_plan_linear_i8", "dllmc_plan_attention_kv4", "dllmc_plan_attention_weights",
 )
 NUM_KERNEL_CLASSES = 13
 
@@ -210,6 +210,8 @@ def lib() -> C.CDLL:
                 ("dllmc_i8_row_bytes", size, [i32]),
                 ("dllmc_op_quant8", C.c_int, [i32, ptr, ptr, i32, i32, ptr, ptr, ptr]),
                 ("dllmc_op_linear_i8_scratch_bytes", size, [i32] * 3),
+                ("dllmc_plan_attention_kv4", i32, [i32] * 7 + [C.POINTER(i32)] * 3),
+                ("dllmc_plan_attention_weights", i32, [i32] * 8 + [C.POINTER(i32)] * 3),
                 ("dllmc_plan_linear_i8", i32, [i32] * 3 + [C.POINTER(i32)] * 3),
                 ("dllmc_op_linear_i8", C.c_int, [i32, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, size, ptr])):
             fn = getattr(L, name)
@@ -684,6 +686,26 @@ def i8_row_bytes(K: int) -> int:
     if n == 0:
         raise DllmcError(f"dllmc_i8_row_bytes: no 8-bit rows of {K}")
     return n
+
+
+def plan_attention_kv4(dtype: str, B: int, Mq: int, n: int, H_q: int, H_kv: int, d_h: int):
+    """(rows and wavefronts of a workgroup, key ranges, tiles that are not cut) of op_attention_kv4; no GPU needed."""
+    rows, waves, whole = C.c_int32(), C.c_int32(), C.c_int32()
+    ks = lib().dllmc_plan_attention_kv4(_DTYPES[dtype][0], B, Mq, n, H_q, H_kv, d_h, C.byref(rows), C.byref(waves), C.byref(whole))
+    if ks < 1:
+        raise DllmcError("dllmc_plan_attention_kv4: invalid argument")
+    return rows.value, waves.value, ks, whole.value
+
+
+def plan_attention_weights(dtype: str, cache_format: str, B: int, Mq: int, n: int, H_q: int, H_kv: int, d_h: int):
+    """(keys a wavefront holds, key ranges of the row sums or 0 where one launch does both, their rows, row shares) of
+    op_attention_weights; no GPU needed."""
+    ranges, rows, shares = C.c_int32(), C.c_int32(), C.c_int32()
+    keys = lib().dllmc_plan_attention_weights(_DTYPES[dtype][0], _format(cache_format), B, Mq, n, H_q, H_kv, d_h, C.byref(ranges),
+                                              C.byref(rows), C.byref(shares))
+    if keys < 1:
+        raise DllmcError("dllmc_plan_attention_weights: invalid argument")
+    return keys, ranges.value, rows.value, shares.value
 
 
 def plan_linear_i8(M: int, N: int, K: int):

@@ -1359,6 +1359,30 @@ int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_
   return DLLMC_OK;
 }
 
+int32_t dllmc_plan_attention_kv4(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv, int32_t d_h, int32_t* rows,
+                                 int32_t* waves, int32_t* whole) {
+  static const int32_t some = 0;
+  if (!dtype_ok(dtype) || !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h)) return DLLMC_EINVAL;
+  const AttendPlan p = plan_attend(dtype, B, Mq, n, H_q, H_kv, d_h);
+  if (rows) *rows = p.rows;
+  if (waves) *waves = p.waves;
+  if (whole) *whole = p.whole;
+  return p.KS;
+}
+
+int32_t dllmc_plan_attention_weights(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv,
+                                     int32_t d_h, int32_t* ranges, int32_t* row_blocks, int32_t* shares) {
+  static const int32_t some = 0;
+  if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) ||
+      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h))
+    return DLLMC_EINVAL;
+  const WeighPlan p = plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+  if (ranges) *ranges = p.brief ? 0 : p.s.KS;
+  if (row_blocks) *row_blocks = p.brief ? 16 : 16 * p.QB;
+  if (shares) *shares = p.s.RS;
+  return 16 * p.KB;
+}
+
 int32_t dllmc_plan_linear_i8(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole) {
   if (M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return DLLMC_EINVAL;
   const I8Plan p = plan_i8(M, N, static_cast<int>(i8_row_bytes(K)));

@@ -130,11 +130,6 @@ template <int D> struct KeyOperand<float, float, D> {
   }
 };
 
-struct WeighShape {
-  int Mq, H_q, H_kv, G, NR;  // NR = Mq * G rows of a KV head
-  int tiles, KS, per;        // stats: tiles of 16 QB rows, key ranges, 32-key blocks per range
-  int blocks, RS, share;     // columns: workgroups of 64 KB keys per head, row shares, 16-row tiles (stages, see there) per share
-};
 __device__ __forceinline__ size_t row_of(const WeighShape& s, int b, int h, int r) {
   const int i = s.G == 1 ? r : r / s.G;
   return (static_cast<size_t>(b) * s.Mq + i) * s.H_q + h * s.G + (r - i * s.G);
@@ -479,7 +474,8 @@ __global__ __launch_bounds__(1024) void k_weigh_sum(const float* __restrict__ pa
 // most 16s of keys a wavefront's registers hold: fragments of at most 128 of them
 constexpr int short_blocks(bool f32_keys, bool f32, int D) { return (f32_keys ? 512 : f32 ? 512 : 1024) / D < 8 ? (f32_keys ? 512 : f32 ? 512 : 1024) / D : 8; }
 
-struct WeighPlan { int QB, KB; bool brief; WeighShape s; };
+}  // namespace
+
 WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
   WeighPlan p{};
   WeighShape& s = p.s;
@@ -522,8 +518,6 @@ WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H
   }
   return p;
 }
-
-}  // namespace
 
 size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
   const WeighPlan p = plan_weigh(dtype, format, B, Mq, n, H_q, H_kv, d_h);

@@ -133,9 +133,19 @@ void launch_kv4_load(int dtype, Kv4Tensor c, int cache_rows, int d_h, const int*
                      hipStream_t st);
 
 // Attention over a 4-bit cache, and the weights that cached positions get; scratch as large as the functions say.
+// rows of an item (16, 32: few; 128, 256: tile), wavefronts, and how many items are not cut
+struct AttendPlan { int rows, waves, tiles, whole, KS, per; long long items; };
+AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h);
 size_t attention_kv4_scratch_bytes(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h);
 void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
                           int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st);
+struct WeighShape {
+  int Mq, H_q, H_kv, G, NR;  // NR = Mq * G rows of a KV head
+  int tiles, KS, per;        // stats: tiles of 16 QB rows, key ranges, 32-key blocks per range
+  int blocks, RS, share;     // columns: workgroups of 64 KB keys per head, row shares, stages (brief: 16-row tiles) per share
+};
+struct WeighPlan { int QB, KB; bool brief; WeighShape s; };
+WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h);
 size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h);
 void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
                               int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,

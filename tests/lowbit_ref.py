@@ -160,3 +160,48 @@ def quant8(x):
         scale[i] = np.float32(top / np.float32(127))
         q[i] = np.rint(row * np.float32(np.float32(127) / top)).astype(np.int64)
     return q, scale
+
+
+def attend_device(q, k, v, where, H_q, H_kv, d_h):
+    """As attend, in float64 on the GPU for larger shapes.  q, k, v: float64 CUDA tensors of attend's shapes.  Returns out, lse, mass,
+    reach (numpy) and columns(rel [B, Mq, H_q]) -> (sum of p, sum of p * rel) per sequence's keys."""
+    B, Mq = q.shape[:2]
+    out = torch.zeros(B, Mq, H_q, d_h, dtype=torch.float64, device="cuda")
+    mass = torch.zeros_like(out)
+    lse = torch.full((B, Mq, H_q), -torch.inf, dtype=torch.float64, device="cuda")
+    reach = torch.zeros(B, Mq, H_q, dtype=torch.float64, device="cuda")
+
+    def probs(b, a):
+        rows = torch.from_numpy(where[b][1]).cuda()
+        kh = k[rows, a // (H_q // H_kv)]
+        s = q[b, :, a] @ kh.t().contiguous() / d_h ** 0.5
+        return s, kh, rows
+
+    for b in range(B):
+        if len(where[b][1]) == 0:
+            continue
+        for a in range(H_q):
+            s, kh, rows = probs(b, a)
+            lse[b, :, a] = torch.logsumexp(s, 1)
+            reach[b, :, a] = (q[b, :, a].abs() @ kh.abs().t().contiguous() / d_h ** 0.5).amax(1)
+            if v is not None:
+                p = torch.exp(s - lse[b, :, a, None])
+                vh = v[rows, a // (H_q // H_kv)].contiguous()
+                out[b, :, a] = p @ vh
+                mass[b, :, a] = p @ vh.abs()
+
+    def columns(rel):
+        rel = torch.from_numpy(rel).cuda()
+        want, tol = [], []
+        for b in range(B):
+            n = len(where[b][1])
+            w, t = torch.zeros(n, dtype=torch.float64, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+            for a in range(H_q if n else 0):
+                p = torch.exp(probs(b, a)[0] - lse[b, :, a, None])
+                w += p.sum(0)
+                t += (p * rel[b, :, a, None]).sum(0)
+            want.append(w.cpu().numpy())
+            tol.append(t.cpu().numpy())
+        return want, tol
+
+    return out.cpu().numpy(), lse.cpu().numpy(), mass.cpu().numpy(), reach.cpu().numpy(), columns
