@@ -8,6 +8,7 @@ fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -563,6 +564,12 @@ def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=4096)
+def _scratch_bytes(what: str, *shape: int) -> int:
+    """dllmc_op_<what>_scratch_bytes, a function of its arguments alone (the choice of a kernel takes a microsecond or two)."""
+    return getattr(lib(), f"dllmc_op_{what}_scratch_bytes")(*shape)
+
+
 def _scratch(nbytes: int) -> Optional[torch.Tensor]:
     return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
 
@@ -577,6 +584,7 @@ def _format(fmt: str) -> int:
     return DLLMC_KV4 if fmt == "kv4" else _DTYPES[fmt][0]
 
 
+@functools.lru_cache(maxsize=1024)
 def kv4_bytes(cache_rows: int, H: int, d_h: int) -> int:
     """Bytes of a 4-bit cache tensor (a uint8 tensor of that size holds it)."""
     n = lib().dllmc_kv4_bytes(cache_rows, H, d_h)
@@ -620,7 +628,7 @@ def op_attention_kv4(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache
     lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
     out = torch.empty_like(q)
     lse = torch.empty((B, Mq, H_q), dtype=torch.float32, device="cuda") if with_lse else None
-    nbytes = lib().dllmc_op_attention_kv4_scratch_bytes(code, B, Mq, n, H_q, H_kv, d_h)
+    nbytes = _scratch_bytes("attention_kv4", code, B, Mq, n, H_q, H_kv, d_h)
     scratch = _scratch(nbytes)
     _check(lib().dllmc_op_attention_kv4(code, qp, B, Mq, kp, vp, cache_rows, rp, lp, n, H_q, H_kv, d_h, out.data_ptr(),
                                         _ptr(lse), _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_kv4")
@@ -643,7 +651,7 @@ def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache
     if out is None:
         out = torch.empty((B, n), dtype=torch.float32, device="cuda")
     op = _need("out", out, torch.float32, (B, n))
-    nbytes = lib().dllmc_op_attention_weights_scratch_bytes(code, fmt, B, Mq, n, H_q, H_kv, d_h)
+    nbytes = _scratch_bytes("attention_weights", code, fmt, B, Mq, n, H_q, H_kv, d_h)
     scratch = _scratch(nbytes)
     _check(lib().dllmc_op_attention_weights(code, fmt, qp, B, Mq, kp, cache_rows, rp, lp, n, H_q, H_kv, d_h, sp, ap, op,
                                             _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_weights")
@@ -680,6 +688,7 @@ def op_compact(cache_format: str, rows: torch.Tensor, src_rows: int, H: int, d_h
            "dllmc_op_compact")
 
 
+@functools.lru_cache(maxsize=1024)
 def i8_row_bytes(K: int) -> int:
     """Bytes of a row of K 8-bit integers: K rounded up to 128."""
     n = lib().dllmc_i8_row_bytes(K)
@@ -737,7 +746,7 @@ def op_linear_i8(dtype: str, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Te
     ap, wp = _need("a", a, torch.int8, (M, kp)), _need("w", w, torch.int8, (N, kp))
     sa, sw = _need("a_scale", a_scale, torch.float32, (M,)), _need("w_scale", w_scale, torch.float32, (N,))
     out = torch.empty((M, N), dtype=tdt, device="cuda")
-    nbytes = lib().dllmc_op_linear_i8_scratch_bytes(M, N, K)
+    nbytes = _scratch_bytes("linear_i8", M, N, K)
     scratch = _scratch(nbytes)
     _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream_handle()),
            "dllmc_op_linear_i8")

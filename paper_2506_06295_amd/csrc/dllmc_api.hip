@@ -1231,7 +1231,7 @@ size_t dllmc_op_attention_kv4_scratch_bytes(int32_t dtype, int32_t B, int32_t Mq
                                             int32_t d_h) {
   static const int32_t some = 0;
   if (!dtype_ok(dtype) || !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h)) return 0;
-  return attention_kv4_scratch_bytes(dtype, B, Mq, n, H_q, H_kv, d_h);
+  return attention_kv4_scratch_bytes(plan_attend(dtype, B, Mq, n, H_q, H_kv, d_h), d_h);
 }
 
 int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, const void* k_cache, const void* v_cache,
@@ -1241,7 +1241,8 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
       !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !aligned16(q) || !aligned16(k_cache) ||
       !aligned16(v_cache) || !aligned16(out) || !aligned4(lse) || !aligned16(scratch))
     return DLLMC_EINVAL;
-  const size_t need = attention_kv4_scratch_bytes(dtype, B, Mq, n, H_q, H_kv, d_h);
+  const AttendPlan plan = plan_attend(dtype, B, Mq, n, H_q, H_kv, d_h);
+  const size_t need = attention_kv4_scratch_bytes(plan, d_h);
   const size_t rows = static_cast<size_t>(B) * Mq * H_q, qb = rows * d_h * elem_bytes(dtype), cb = kv4_bytes(cache_rows, H_kv, d_h);
   const struct { const void* p; size_t n; } in[] = {{q, qb}, {k_cache, cb}, {v_cache, cb},
                                                     {row_map, row_map ? static_cast<size_t>(B) * n * 4 : 0}, {lens, lens ? static_cast<size_t>(B) * 4 : 0}};
@@ -1250,7 +1251,7 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
     if (i.n && (!apart(out, qb, i.p, i.n) || (lse && !apart(lse, rows * 4, i.p, i.n)))) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
   (void)hipGetLastError();
-  launch_attention_kv4(dtype, q, B, Mq, cache_view(DLLMC_KV4, k_cache, cache_rows, H_kv, d_h),
+  launch_attention_kv4(plan, dtype, q, Mq, cache_view(DLLMC_KV4, k_cache, cache_rows, H_kv, d_h),
                        cache_view(DLLMC_KV4, v_cache, cache_rows, H_kv, d_h), Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, out,
                        lse, scratch, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
@@ -1263,7 +1264,7 @@ size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_for
   if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) ||
       !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h))
     return 0;
-  return attention_weights_scratch_bytes(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+  return attention_weights_scratch_bytes(plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h), B, Mq, n, H_q, H_kv);
 }
 
 int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* q, int32_t B, int32_t Mq, const void* k_cache,
@@ -1274,7 +1275,8 @@ int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* 
       !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !aligned16(q) || !aligned16(k_cache) ||
       !aligned4(lse) || !aligned4(acc_in) || !aligned4(acc_out) || !aligned16(scratch))
     return DLLMC_EINVAL;
-  const size_t need = attention_weights_scratch_bytes(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+  const WeighPlan plan = plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
+  const size_t need = attention_weights_scratch_bytes(plan, B, Mq, n, H_q, H_kv);
   const size_t rows = static_cast<size_t>(B) * Mq * H_q, ob = static_cast<size_t>(B) * n * 4;
   const struct { const void* p; size_t n; } in[] = {{q, rows * d_h * elem_bytes(dtype)}, {k_cache, cache_bytes(cache_format, cache_rows, H_kv, d_h)},
                                                     {row_map, row_map ? ob : 0}, {lens, lens ? static_cast<size_t>(B) * 4 : 0},
@@ -1283,7 +1285,7 @@ int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* 
     if (i.n && !apart(acc_out, ob, i.p, i.n)) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
   (void)hipGetLastError();
-  launch_attention_weights(dtype, cache_format, q, B, Mq, cache_view(cache_format, k_cache, cache_rows, H_kv, d_h),
+  launch_attention_weights(plan, dtype, cache_format, q, B, Mq, cache_view(cache_format, k_cache, cache_rows, H_kv, d_h),
                            Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, lse, acc_in, acc_out, scratch,
                            static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
@@ -1394,7 +1396,7 @@ int32_t dllmc_plan_linear_i8(int32_t M, int32_t N, int32_t K, int32_t* cols, int
 
 size_t dllmc_op_linear_i8_scratch_bytes(int32_t M, int32_t N, int32_t K) {
   if (M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 || K > kMaxI8K) return 0;
-  return linear_i8_scratch_bytes(M, N, K);
+  return linear_i8_scratch_bytes(plan_i8(M, N, static_cast<int>(i8_row_bytes(K))), M, N);
 }
 
 int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int32_t M, const int8_t* w, const float* w_scale,
@@ -1403,14 +1405,16 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
       K > kMaxI8K || !aligned16(a) || !aligned16(w) || !aligned4(a_scale) || !aligned4(w_scale) ||
       reinterpret_cast<uintptr_t>(out) % elem_bytes(dtype) || !aligned16(scratch))
     return DLLMC_EINVAL;
-  const size_t need = linear_i8_scratch_bytes(M, N, K), kp = i8_row_bytes(K);
+  const size_t kp = i8_row_bytes(K);
+  const I8Plan plan = plan_i8(M, N, static_cast<int>(kp));
+  const size_t need = linear_i8_scratch_bytes(plan, M, N);
   const size_t ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
   if (!apart(out, ob, a, M * kp) || !apart(out, ob, w, N * kp) || !apart(out, ob, a_scale, static_cast<size_t>(M) * 4) ||
       !apart(out, ob, w_scale, static_cast<size_t>(N) * 4))
     return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
   (void)hipGetLastError();
-  launch_linear_i8(dtype, a, a_scale, M, w, w_scale, N, K, out, scratch, static_cast<hipStream_t>(hip_stream));
+  launch_linear_i8(plan, dtype, a, a_scale, M, w, w_scale, N, K, out, scratch, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
   return DLLMC_OK;
 }

@@ -661,8 +661,56 @@ constexpr AttendCost kAttendCosts[] = {
     {256, 0, 16, 4, 2, 2.76, 1.5, 0.9, 0.84, 0.03, 3.09, 0.329, 0.202},
     {256, 1, 16, 4, 1, 2.78, 1.5, 2.4, 0, 0.03, 2.68, 0.521, 0.268},
 };
-void launch_plan(const AttendPlan& p, int dtype, const void* q, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
-                 int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st) {
+}  // namespace
+
+AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
+  const int NR = Mq * (H_q / H_kv);
+  const double mb = 2.0 * B * n * H_kv * (d_h / 2 + d_h / 32) / 1e6;
+  AttendPlan best{};
+  double best_t = 1e300;
+  for (const AttendCost& c : kAttendCosts) {
+    if (c.d != d_h || c.f32 != (dtype == 0)) continue;
+    AttendPlan p{};
+    const bool tile = c.rows >= 128;
+    p.rows = c.rows;
+    p.waves = c.waves;
+    p.tiles = (NR + c.rows - 1) / c.rows;
+    p.items = static_cast<long long>(B) * H_kv * p.tiles;
+    const int blocks = (n + (tile ? 63 : 31)) / (tile ? 64 : 32), deal = tile ? 1 : c.waves;
+    const long long slots = 256ll * c.groups;
+    auto up = [](long long x, long long y) { return static_cast<double>((x + y - 1) / y); };
+    for (const int ks : {1, 2, 3, 4, 6, 8, 10, 12, 16, 24, 32, 48, 64}) {
+      if (ks > blocks) break;
+      const int per = (blocks + ks - 1) / ks, used = (blocks + per - 1) / per;
+      if (used != ks) continue;
+      // all items whole; all cut; tiles: those beyond the last whole round cut
+      for (int w = 0; w < (ks == 1 ? 1 : tile ? 2 : 1); ++w) {
+        const long long whole = ks == 1 ? p.items : w == 0 ? 0 : p.items / slots * slots, cut = p.items - whole;
+        if (ks > 1 && cut == 0) continue;
+        const double steps = up(blocks, deal), part_steps = up(per, deal);
+        double t = c.start + (up(whole, slots) + up(cut * ks, slots)) * c.round +
+                   (up(whole, slots) * steps + up(cut * ks, slots) * part_steps) * c.block +
+                   (up(whole, 256) * steps + up(cut * ks, 256) * part_steps) * c.share + mb * c.mb;
+        if (cut > 0) t += c.cut + static_cast<double>(cut) * c.rows * ks * (d_h + 2) * 4e-6 * c.part + ks * c.range;
+        if (t < best_t) {
+          best_t = t;
+          best = p;
+          best.whole = static_cast<int>(whole);
+          best.KS = ks;
+          best.per = per;
+        }
+      }
+    }
+  }
+  return best;
+}
+
+size_t attention_kv4_scratch_bytes(const AttendPlan& p, int d_h) {
+  return static_cast<size_t>(p.items - p.whole) * p.rows * p.KS * (d_h + 2) * sizeof(float);
+}
+
+void launch_attention_kv4(const AttendPlan& p, int dtype, const void* q, int Mq, const CacheView& k, const CacheView& v, const Keys& keys,
+                          int H_q, int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st) {
   const AttendShape s{Mq, H_q, H_kv, H_q / H_kv, Mq * (H_q / H_kv), p.tiles, p.whole, p.KS, p.per};
   const long long cut = p.items - p.whole;
   float* part = static_cast<float*>(scratch);
@@ -703,59 +751,6 @@ void launch_plan(const AttendPlan& p, int dtype, const void* q, int Mq, const Ca
     if (dtype == 1) with_d(bf16_t(), std::false_type{});
     else with_d(float(), std::false_type{});
   }
-}
-
-}  // namespace
-
-AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
-  const int NR = Mq * (H_q / H_kv);
-  const double mb = 2.0 * B * n * H_kv * (d_h / 2 + d_h / 32) / 1e6;
-  AttendPlan best{};
-  double best_t = 1e300;
-  for (const AttendCost& c : kAttendCosts) {
-    if (c.d != d_h || c.f32 != (dtype == 0)) continue;
-    AttendPlan p{};
-    const bool tile = c.rows >= 128;
-    p.rows = c.rows;
-    p.waves = c.waves;
-    p.tiles = (NR + c.rows - 1) / c.rows;
-    p.items = static_cast<long long>(B) * H_kv * p.tiles;
-    const int blocks = (n + (tile ? 63 : 31)) / (tile ? 64 : 32), deal = tile ? 1 : c.waves;
-    const long long slots = 256ll * c.groups;
-    auto up = [](long long x, long long y) { return static_cast<double>((x + y - 1) / y); };
-    for (int ks = 1; ks <= 64; ks += ks < 4 ? 1 : ks < 12 ? 2 : 4) {
-      const int per = (blocks + ks - 1) / ks, used = (blocks + per - 1) / per;
-      if (used != ks) continue;
-      // all items whole; all cut; tiles: those beyond the last whole round cut
-      for (int w = 0; w < (ks == 1 ? 1 : tile ? 2 : 1); ++w) {
-        const long long whole = ks == 1 ? p.items : w == 0 ? 0 : p.items / slots * slots, cut = p.items - whole;
-        if (ks > 1 && cut == 0) continue;
-        const double steps = up(blocks, deal), part_steps = up(per, deal);
-        double t = c.start + (up(whole, slots) + up(cut * ks, slots)) * c.round +
-                   (up(whole, slots) * steps + up(cut * ks, slots) * part_steps) * c.block +
-                   (up(whole, 256) * steps + up(cut * ks, 256) * part_steps) * c.share + mb * c.mb;
-        if (cut > 0) t += c.cut + static_cast<double>(cut) * c.rows * ks * (d_h + 2) * 4e-6 * c.part + ks * c.range;
-        if (t < best_t) {
-          best_t = t;
-          best = p;
-          best.whole = static_cast<int>(whole);
-          best.KS = ks;
-          best.per = per;
-        }
-      }
-    }
-  }
-  return best;
-}
-
-size_t attention_kv4_scratch_bytes(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
-  const AttendPlan p = plan_attend(dtype, B, Mq, n, H_q, H_kv, d_h);
-  return static_cast<size_t>(p.items - p.whole) * p.rows * p.KS * (d_h + 2) * sizeof(float);
-}
-
-void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
-                          int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st) {
-  launch_plan(plan_attend(dtype, B, Mq, keys.n, H_q, H_kv, d_h), dtype, q, Mq, k, v, keys, H_q, H_kv, d_h, out, lse, scratch, st);
 }
 
 }  // namespace dllmc

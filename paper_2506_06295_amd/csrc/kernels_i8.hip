@@ -580,15 +580,13 @@ void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8
   else quant8(static_cast<const float*>(x), rows, M, K, q, scale, st);
 }
 
-size_t linear_i8_scratch_bytes(int M, int N, int K) {
-  const I8Plan p = plan_i8(M, N, static_cast<int>(i8_row_bytes(K)));
+size_t linear_i8_scratch_bytes(const I8Plan& p, int M, int N) {
   return p.S == 1 ? 0 : static_cast<size_t>(p.S) * M * N * sizeof(int);
 }
 
-void launch_linear_i8(int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale, int N, int K,
-                      void* out, void* scratch, hipStream_t st) {
+void launch_linear_i8(const I8Plan& p, int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale,
+                      int N, int K, void* out, void* scratch, hipStream_t st) {
   const int Kp = static_cast<int>(i8_row_bytes(K));
-  const I8Plan p = plan_i8(M, N, Kp);
   if (dtype == 1) launch_i8(p, a, a_scale, M, w, w_scale, N, Kp, static_cast<bf16_t*>(out), static_cast<int*>(scratch), st);
   else launch_i8(p, a, a_scale, M, w, w_scale, N, Kp, static_cast<float*>(out), static_cast<int*>(scratch), st);
 }

@@ -2,9 +2,10 @@
 //
 // A row's probabilities need its maximum and sum before any column can be added up.  Up to 1024 keys k_weigh_short holds a head's
 // keys in the registers of one workgroup and forms every score once.  Beyond, scores are formed twice: k_weigh_stats reduces every row over
-// ranges of keys to (m, l), k_weigh_join those to z = m + log2 l, and k_weigh_cols holds a block of keys in registers, walks the rows and
-// adds exp2(s - z) per key; where the caller has the rows' log-sum-exp, the first two and their pass over the keys fall
-// away.  k_weigh_sum adds what heads and row shares left, in their order.  No value is read and no probability leaves a register.
+// ranges of keys to (m, l), k_weigh_join joins those, and k_weigh_cols holds a block of keys in registers, walks the rows and
+// adds exp2(s - m) / l per key (exp2(s - m - log2 l) would round an exponent of 10 to 2^-21); where the caller has the rows'
+// log-sum-exp, the first two and their pass over the keys fall away.  k_weigh_sum adds what heads and row shares left, in their order.
+// No value is read and no probability leaves a register.
 #include <type_traits>
 
 #include "kv4.hpp"
@@ -135,14 +136,15 @@ __device__ __forceinline__ size_t row_of(const WeighShape& s, int b, int h, int 
   return (static_cast<size_t>(b) * s.Mq + i) * s.H_q + h * s.G + (r - i * s.G);
 }
 
-// (m, l) of 16 QB rows over a range of keys, base 2, or z where the range is all of them; the eight wavefronts deal the range's blocks
+// (m, l) of 16 QB rows over a range of keys, base 2, or m and 1 / l where the range is all of them; the eight wavefronts deal the range's blocks
 // of 32 keys, the next one in flight.  Bound by vector instructions (one per 5 cycles: 4.5 a score) and the products
 // beside them: 0.66 of what the products alone would take, 4608 rows x 4608 keys x 32 heads.
 constexpr int kSW = 8;
 template <typename F, typename T, int D, int QB>
 __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_stats(const T* __restrict__ q, WeighShape s, CacheView k,
                                                                                             Keys keys, float2* __restrict__ ml,
-                                                                                            float* __restrict__ z) {
+                                                                                            float* __restrict__ m_out,
+                                                                                            float* __restrict__ il_out) {
   typedef KeyOperand<F, T, D> Op;
   __shared__ float2 hand[kSW][16 * QB];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
@@ -246,13 +248,18 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (int w = 1; w < kSW; ++w) v = join(v, hand[w][threadIdx.x]);
     const size_t w = row_of(s, b, h, r0 + threadIdx.x);
-    if (s.KS == 1) z[w] = v.x + log2f(v.y);
-    else ml[w * s.KS + range] = v;
+    if (s.KS == 1) {
+      m_out[w] = v.x;
+      il_out[w] = 1.f / v.y;
+    } else {
+      ml[w * s.KS + range] = v;
+    }
   }
 }
 
-// z = m + log2 l over the ranges, one thread per row
-__global__ __launch_bounds__(256) void k_weigh_join(const float2* __restrict__ ml, int KS, int rows, float* __restrict__ z) {
+// m and 1 / l over the ranges, one thread per row
+__global__ __launch_bounds__(256) void k_weigh_join(const float2* __restrict__ ml, int KS, int rows, float* __restrict__ m_out,
+                                                    float* __restrict__ il_out) {
   const int w = blockIdx.x * 256 + threadIdx.x;
   if (w >= rows) return;
   float m = -INFINITY, l = 0.f;
@@ -262,7 +269,8 @@ __global__ __launch_bounds__(256) void k_weigh_join(const float2* __restrict__ m
     l = (l != l ? l : l * __builtin_amdgcn_exp2f(m - u)) + (c.y != c.y ? c.y : c.y * __builtin_amdgcn_exp2f(c.x - u));
     m = M;
   }
-  z[w] = m + log2f(l);
+  m_out[w] = m;
+  il_out[w] = 1.f / l;
 }
 
 // 16 KB column sums of a wavefront leave for part[j], zero where there is no key; `there`: keys of each 16
@@ -295,7 +303,7 @@ __device__ __forceinline__ void load_keys(const CacheView& k, const Keys& keys, 
 }
 
 // Column sums: a wavefront holds 16 KB keys of one KV head and walks its share of the head's rows; rows come in stages of 8 KB (16
-// rows at least) through a ring in LDS that the four wavefronts share, with their z.  part[(share * B + b) * H_kv + h][n].
+// rows at least) through a ring in LDS that the four wavefronts share, with their m and 1 / l (lse: mul * m, no l).  part[(share * B + b) * H_kv + h][n].
 // With every wavefront fetching its rows by itself, 16 ahead, a launch of 512 rows x 4608 keys x 32 heads waited on trips to the L2: 60 us.
 template <typename T, int D> struct WeighStage {
   static constexpr int kRow = D * static_cast<int>(sizeof(T)), kRows = kRow >= 512 ? 16 : 8192 / kRow;
@@ -303,11 +311,13 @@ template <typename T, int D> struct WeighStage {
 };
 template <typename F, typename T, int D, int KB>
 __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const WeighShape& s, const CacheView& k, const Keys& keys,
-                                                const float* __restrict__ z, float zmul, float* __restrict__ part) {
+                                                const float* __restrict__ m, const float* __restrict__ il, float mul,
+                                                float* __restrict__ part) {
   typedef KeyOperand<F, T, D> Op;
   typedef WeighStage<T, D> St;
+  constexpr int kIssued = St::kLoads + 2;
   constexpr int NS = St::kStages, kChunks = St::kRow / 16, kMix = kChunks < 16 ? kChunks : 16;
-  __shared__ __attribute__((aligned(1024))) uint4 lds[NS * St::kVecs + NS * 4 * 16];
+  __shared__ __attribute__((aligned(1024))) uint4 lds[NS * St::kVecs + NS * 4 * 32];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
   int x = xcd_group_item(blockIdx.x, gridDim.x, s.blocks);  // key blocks of one head and share read the same rows
@@ -319,7 +329,8 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
   float* out = part + (static_cast<size_t>(share * B + b) * s.H_kv + h) * keys.n;
   const int t0 = share * s.share, t1 = min((s.NR + St::kRows - 1) / St::kRows, t0 + s.share);
 
-  // loader: instruction j of a stage copies 1 KB, wavefront w issues kLoads w .. + kLoads - 1 and its own copy of z
+  // loader: instruction j of a stage copies 1 KB, wavefront w issues kLoads w .. + kLoads - 1 and its own copy of m and 1 / l
+  const float* second = il != nullptr ? il : m;
   auto issue = [&](int slot, int t) {
 #pragma unroll
     for (int j = 0; j < St::kLoads; ++j) {
@@ -329,7 +340,8 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
                                        16, 0, 0);
     }
     const size_t w = row_of(s, b, h, min(t * St::kRows + lane % St::kRows, s.NR - 1));
-    __builtin_amdgcn_global_load_lds(z + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 16], 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(m + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32], 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(second + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32 + 16], 4, 0, 0);
   };
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
@@ -344,8 +356,8 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
   int slot = 0;
   for (int t = t0; t < t1; ++t) {
     const int rem = t1 - 1 - t;
-    if (rem >= NS - 2) wait_vmcnt_lds<(NS - 2) * (St::kLoads + 1)>();
-    else if (rem == 1) wait_vmcnt_lds<St::kLoads + 1>();
+    if (rem >= NS - 2) wait_vmcnt_lds<(NS - 2) * kIssued>();
+    else if (rem == 1) wait_vmcnt_lds<kIssued>();
     else wait_vmcnt_lds<0>();
     __builtin_amdgcn_s_barrier();  // stage t is there for everybody, and everybody has read stage t - 1, which is filled next
     if (t + NS - 1 < t1) issue(slot == 0 ? NS - 1 : slot - 1, t + NS - 1);
@@ -353,15 +365,17 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
 #pragma unroll
       for (int g = 0; g < St::kRows / 16; ++g) {
         const int r = g * 16 + ln;
-        float zr = reinterpret_cast<const float*>(&lds[NS * St::kVecs + (slot * 4 + wave) * 16])[r] * zmul;
-        if (t * St::kRows + r >= s.NR) zr = INFINITY;  // rows past the last one weigh nothing
+        const float* row = reinterpret_cast<const float*>(&lds[NS * St::kVecs + (slot * 4 + wave) * 32]) + r;
+        float mr = row[0] * mul;
+        const float ir = il != nullptr ? row[64] : 1.f;
+        if (t * St::kRows + r >= s.NR) mr = INFINITY;  // rows past the last one weigh nothing
         typename Op::Query qf;
         Op::query_pieces([&](int c) { return lds[slot * St::kVecs + r * kChunks + (c ^ (r % kMix))]; }, lg, qf);
 #pragma unroll
         for (int u = 0; u < KB; ++u) {
           const f32x4 st = Op::scores(kf[u], qf);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum[u][e] += __builtin_amdgcn_exp2f(fmaf(st[e], sl2e, -zr));
+          for (int e = 0; e < 4; ++e) sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(st[e], sl2e, -mr)), ir, sum[u][e]);
         }
       }
     }
@@ -371,9 +385,10 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
 }
 template <typename F, typename T, int D, int KB>
 __global__ __launch_bounds__(256, D == 256 && sizeof(T) == 4 ? 1 : 2) void k_weigh_cols(const T* __restrict__ q, WeighShape s, CacheView k,
-                                                                                 Keys keys, const float* __restrict__ z, float zmul,
+                                                                                 Keys keys, const float* __restrict__ m,
+                                                                                 const float* __restrict__ il, float mul,
                                                                                  float* __restrict__ part) {
-  weigh_cols_body<F, T, D, KB>(q, s, k, keys, z, zmul, part);
+  weigh_cols_body<F, T, D, KB>(q, s, k, keys, m, il, mul, part);
 }
 
 // Up to 128 KB keys: the eight wavefronts of a workgroup hold them all, 16 KB each, and walk a share of the head's rows 16 at a time.
@@ -519,20 +534,19 @@ WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H
   return p;
 }
 
-size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
-  const WeighPlan p = plan_weigh(dtype, format, B, Mq, n, H_q, H_kv, d_h);
+size_t attention_weights_scratch_bytes(const WeighPlan& p, int B, int Mq, int n, int H_q, int H_kv) {
   const size_t rows = static_cast<size_t>(B) * Mq * H_q;
-  return (p.brief ? 0 : (rows * (2 * p.s.KS + 1) + 1) / 2 * 2 * sizeof(float)) + static_cast<size_t>(p.s.RS) * B * H_kv * n * sizeof(float);
+  return (p.brief ? 0 : rows * (2 * p.s.KS + 2) * sizeof(float)) + static_cast<size_t>(p.s.RS) * B * H_kv * n * sizeof(float);
 }
 
-namespace {
-void launch_weigh(const WeighPlan& p, int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
-                  int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch, hipStream_t st) {
+void launch_attention_weights(const WeighPlan& p, int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys,
+                              int H_q, int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch, hipStream_t st) {
   const WeighShape& s = p.s;
   const size_t count = static_cast<size_t>(B) * Mq * H_q;
   float2* ml = static_cast<float2*>(scratch);
-  float* z = static_cast<float*>(scratch) + 2 * s.KS * count;
-  float* part = static_cast<float*>(scratch) + (p.brief ? 0 : (count * (2 * s.KS + 1) + 1) / 2 * 2);
+  float* m = static_cast<float*>(scratch) + 2 * s.KS * count;
+  float* il = m + count;
+  float* part = static_cast<float*>(scratch) + (p.brief ? 0 : count * (2 * s.KS + 2));
   auto go = [&](auto f, auto t, auto d) {
     typedef decltype(f) F;
     typedef decltype(t) T;
@@ -554,19 +568,19 @@ void launch_weigh(const WeighPlan& p, int dtype, int format, const void* q, int 
     if (lse == nullptr) {
       const dim3 rows(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.tiles * s.KS));
       if constexpr (f32 || D == 256) {
-        hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+        hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, m, il);
       } else {
-        if (p.QB == 1) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
-        else if (p.QB == 2) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 2>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
-        else hipLaunchKernelGGL((k_weigh_stats<F, T, D, 4>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, z);
+        if (p.QB == 1) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 1>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, m, il);
+        else if (p.QB == 2) hipLaunchKernelGGL((k_weigh_stats<F, T, D, 2>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, m, il);
+        else hipLaunchKernelGGL((k_weigh_stats<F, T, D, 4>), rows, dim3(64 * kSW), 0, st, qt, s, k, keys, ml, m, il);
       }
       if (s.KS > 1)
         hipLaunchKernelGGL(k_weigh_join, dim3(static_cast<unsigned>((count + 255) / 256)), dim3(256), 0, st, ml, s.KS, static_cast<int>(count),
-                         z);
+                           m, il);
     }
     constexpr int KB = f32_keys || D == 256 ? 2 : 4;
     hipLaunchKernelGGL((k_weigh_cols<F, T, D, KB>), dim3(static_cast<unsigned>(static_cast<long long>(B) * H_kv * s.blocks * s.RS)),
-                       dim3(256), 0, st, qt, s, k, keys, lse ? lse : z, lse ? kLog2e : 1.f, part);
+                       dim3(256), 0, st, qt, s, k, keys, lse ? lse : m, lse ? nullptr : il, lse ? kLog2e : 1.f, part);
   };
   auto with_d = [&](auto f, auto t) {
     if (d_h == 64) go(f, t, std::integral_constant<int, 64>{});
@@ -583,15 +597,6 @@ void launch_weigh(const WeighPlan& p, int dtype, int format, const void* q, int 
   }
   hipLaunchKernelGGL(k_weigh_sum, dim3(static_cast<unsigned>(B * ((keys.n + 63) / 64))), dim3(1024), 0, st, part, s.RS, B, H_kv, keys.n,
                      acc_in, acc_out);
-}
-
-}  // namespace
-
-void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
-                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
-                              hipStream_t st) {
-  launch_weigh(plan_weigh(dtype, format, B, Mq, keys.n, H_q, H_kv, d_h), dtype, format, q, B, Mq, k, keys, H_q, H_kv, d_h, lse, acc_in,
-               acc_out, scratch, st);
 }
 
 }  // namespace dllmc

@@ -136,9 +136,9 @@ void launch_kv4_load(int dtype, Kv4Tensor c, int cache_rows, int d_h, const int*
 // rows of an item (16, 32: few; 128, 256: tile), wavefronts, and how many items are not cut
 struct AttendPlan { int rows, waves, tiles, whole, KS, per; long long items; };
 AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h);
-size_t attention_kv4_scratch_bytes(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h);
-void launch_attention_kv4(int dtype, const void* q, int B, int Mq, const CacheView& k, const CacheView& v, const Keys& keys, int H_q,
-                          int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st);
+size_t attention_kv4_scratch_bytes(const AttendPlan& p, int d_h);
+void launch_attention_kv4(const AttendPlan& p, int dtype, const void* q, int Mq, const CacheView& k, const CacheView& v, const Keys& keys,
+                          int H_q, int H_kv, int d_h, void* out, float* lse, void* scratch, hipStream_t st);
 struct WeighShape {
   int Mq, H_q, H_kv, G, NR;  // NR = Mq * G rows of a KV head
   int tiles, KS, per;        // stats: tiles of 16 QB rows, key ranges, 32-key blocks per range
@@ -146,9 +146,9 @@ struct WeighShape {
 };
 struct WeighPlan { int QB, KB; bool brief; WeighShape s; };
 WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h);
-size_t attention_weights_scratch_bytes(int dtype, int format, int B, int Mq, int n, int H_q, int H_kv, int d_h);
-void launch_attention_weights(int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys, int H_q,
-                              int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
+size_t attention_weights_scratch_bytes(const WeighPlan& p, int B, int Mq, int n, int H_q, int H_kv);
+void launch_attention_weights(const WeighPlan& p, int dtype, int format, const void* q, int B, int Mq, const CacheView& k, const Keys& keys,
+                              int H_q, int H_kv, int d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
                               hipStream_t st);
 
 // Which positions stay (kernels_evict.hip), and rows moved: dst row i = src row rows[i] for i < M where that is one.
@@ -162,8 +162,8 @@ inline size_t i8_row_bytes(int K) { return (static_cast<size_t>(K) + 127) / 128 
 void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st);
 struct I8Plan { int wide, bm, bn, S, per; };  // wide: tile kernel; else ring of bm x bn and S slices of `per` bytes
 I8Plan plan_i8(int M, int N, int Kp);
-size_t linear_i8_scratch_bytes(int M, int N, int K);
-void launch_linear_i8(int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale, int N, int K,
-                      void* out, void* scratch, hipStream_t st);
+size_t linear_i8_scratch_bytes(const I8Plan& p, int M, int N);
+void launch_linear_i8(const I8Plan& p, int dtype, const int8_t* a, const float* a_scale, int M, const int8_t* w, const float* w_scale,
+                      int N, int K, void* out, void* scratch, hipStream_t st);
 
 }  // namespace dllmc
