@@ -478,24 +478,28 @@ __global__ __launch_bounds__(256, 1) void k_i8_wide(const int8_t* __restrict__ A
 }
 
 // Tile and slices with the lowest estimate, us: start + rounds of 256 workgroups x (round + line x 128-byte columns) + MB of weights x
-// w + MB of results x out, or of int32 sums x sums + the launch that adds them.  Fitted (9 % rms) to 4500 launches, cold
-// weights, 1 to 12288 rows, nine maps of 256 to 18944; the choices are 1.1 % from the quickest shape on average, and the shapes
-// left out of the list (ring 32 x 32, 64 x 32, 128 x 16 and x 32, tiles 64 x 128 and x 256) not 0.1 % more.  Floors: 64 rows x 12288 x 4096
-// 10.5 us of bytes, 15.0 reached (a workgroup takes in 64 rows besides its 48 of the weights: 450 KB a CU at 40 GB/s); one row 10.1 and 10.8;
-// 12288 rows 526 at the rate of a large library product, 509.  Non-temporal weights: 3 % quicker cold up to 16 rows, 6 % slower from a
-// cache, and slower with more rows: not taken.
+// w + MB of results x out, or of int32 sums x sums + the launch that adds them.  Fitted (9 % rms) to 9000 launches, cold
+// weights, 1 to 12288 rows, ten maps of 256 to 18944; the choices are 2.0 % from the quickest of 50 shapes on average.  Of shapes
+// with the same rows those win whose wavefronts share the contraction: a stage is then longer and a barrier feeds more products (64 rows:
+// stages of 256 bytes a row against 128, us: 4096 x 4096 9.6 and 12.1, 12288 x 4096 13.7 and 14.7, 18944 x 3584 16.9 and 24.9).  At 12288 x 4096 one
+// row takes 10.8 us (floor 10.1 of weights), 64 rows 13.7 (10.6: each workgroup takes in 64 rows besides its 48 of the weights, 450 KB
+// a CU), 12288 rows 541 (526 at the rate of a large library product).  Non-temporal
+// weights: 3 % quicker cold up to 16 rows, 6 % slower from a cache, and slower with more rows: not taken.
 struct I8Cost { int wide, bm, bn; double start, round, line, w, out, sums, add; };
 constexpr I8Cost kI8Costs[] = {
-    {0, 16, 16, 1.41, 1.34, 0.068, 0.0501, 3.8, 0.705, 3},      {0, 16, 32, 1.52, 1.41, 0.08, 0.0747, 2.2, 0.656, 3.04},
-    {0, 16, 48, 1.69, 1.62, 0.104, 0.0634, 1.56, 0.307, 3.26},  {0, 16, 64, 1.81, 1.74, 0.126, 0.0901, 0.233, 0.467, 2.5},
-    {0, 32, 16, 1.53, 1.15, 0.148, 0.0137, 2, 0.987, 2.89},     {0, 32, 48, 2.31, 1.85, 0.164, 0.0556, 0.0428, 0.286, 2.23},
-    {0, 32, 64, 1.96, 1.1, 0.179, 0.059, 0.899, 0.753, 2.69},   {0, 64, 16, 2.74, 0.453, 0.172, 0.051, 1.24, 0.534, 2.83},
-    {0, 64, 48, 2.38, 1.27, 0.295, 0.0213, 0.763, 0.595, 2.13}, {0, 64, 64, 2.56, 0.854, 0.28, 0.0401, 0.914, 0.72, 2.36},
-    {0, 128, 48, 3.36, 0.542, 0.35, 0.0209, 0.799, 0.685, 2.03}, {0, 128, 64, 3.34, 0.804, 0.391, 0.0212, 0.702, 0.592, 2.28},
-    {1, 128, 64, 1.7, 1.95, 0.336, 0.0368, 0.161, 0, 0},        {1, 128, 128, 1.35, 3.62, 0.473, 0.054, 0.155, 0, 0},
-    {1, 128, 256, 1.73, 5.31, 0.753, 0.0213, 0.229, 0, 0},      {1, 192, 128, 0.443, 5.27, 0.6, 0.00571, 0.263, 0, 0},
-    {1, 192, 256, 0, 9.01, 0.891, 0.0228, 0.235, 0, 0},         {1, 256, 128, 0.96, 5.56, 0.698, 0.0136, 0.27, 0, 0},
-    {1, 256, 256, 0, 11.1, 1.13, 0.0183, 0.246, 0, 0}};
+    {0, 16, 16, 1.51, 1.32, 0.0652, 0.0579, 3.25, 1.37, 2.42},  {0, 16, 48, 1.52, 1.53, 0.099, 0.0821, 0.934, 0.274, 3.06},
+    {0, 16, 80, 1.55, 1.6, 0.166, 0.0823, 1.15, 0.752, 2.73},   {0, 32, 32, 1.77, 1.43, 0.106, 0.0676, 0.185, 0.631, 2.62},
+    {0, 32, 48, 2.39, 0.807, 0.136, 0.0727, 1.16, 1.04, 2.49},  {0, 32, 64, 1.38, 2.11, 0.176, 0.0585, 0.244, 0.451, 3.02},
+    {0, 32, 80, 1.68, 2.25, 0.296, 0.0603, 0.109, 0.328, 2.71}, {0, 48, 16, 1.59, 1.39, 0.0999, 0.0434, 0.957, 0.927, 2.44},
+    {0, 64, 16, 1.55, 1.46, 0.173, 0.0341, 0.89, 0.59, 2.39},   {0, 64, 32, 1.94, 1.23, 0.179, 0.0289, 0.862, 0.725, 2.51},
+    {0, 64, 48, 2.21, 1.37, 0.206, 0.0484, 0.739, 0.632, 2.36}, {0, 64, 64, 2.03, 1.45, 0.243, 0.0345, 0.614, 0.65, 2.34},
+    {0, 64, 80, 2.4, 1.47, 0.285, 0.0311, 0.781, 0.589, 2.61},  {0, 128, 16, 1.91, 1.08, 0.23, 0.0456, 1.13, 0.84, 2.38},
+    {0, 128, 64, 2.91, 1.71, 0.341, 0.0296, 0.501, 0.6, 2.13},  {0, 128, 80, 3.94, 1.01, 0.438, 0.0144, 0.554, 0.593, 1.7},
+    {1, 128, 64, 1.61, 1.89, 0.33, 0.0389, 0.204, 0, 0},        {1, 128, 128, 1.56, 3.09, 0.471, 0.0541, 0.227, 0, 0},
+    {1, 128, 256, 1.41, 5.64, 0.747, 0.031, 0.215, 0, 0},       {1, 192, 128, 0.588, 5.05, 0.582, 0.0177, 0.308, 0, 0},
+    {1, 192, 256, 0, 8.83, 0.884, 0.023, 0.258, 0, 0},          {1, 256, 128, 1.83, 4.33, 0.676, 0.00491, 0.391, 0, 0},
+    {1, 256, 256, 0.785, 9.57, 1.13, 0.00482, 0.31, 0, 0}};
+
 template <typename T>
 void launch_i8(const I8Plan& p, const int8_t* a, const float* sa, int M, const int8_t* w, const float* sw, int N, int Kp, T* out,
                int* sums, hipStream_t st) {
@@ -519,17 +523,21 @@ void launch_i8(const I8Plan& p, const int8_t* a, const float* sa, int M, const i
   hipLaunchKernelGGL((k_i8_ring<T, RG, RB, NB>), grid, dim3(512), 0, st, a, sa, M, w, sw, N, Kp, p.per, out, sums)
   switch (p.bm * 100 + p.bn) {
     case 1616: DLLMC_R(1, 1, 1); break;
-    case 1632: DLLMC_R(1, 1, 2); break;
     case 1648: DLLMC_R(1, 1, 3); break;
-    case 1664: DLLMC_R(1, 1, 4); break;
-    case 3216: DLLMC_R(2, 1, 1); break;
-    case 3248: DLLMC_R(2, 1, 3); break;
-    case 3264: DLLMC_R(2, 1, 4); break;
-    case 6416: DLLMC_R(4, 1, 1); break;
-    case 6448: DLLMC_R(4, 1, 3); break;
-    case 6464: DLLMC_R(4, 1, 4); break;
-    case 12848: DLLMC_R(4, 2, 3); break;
-    default: DLLMC_R(4, 2, 4); break;
+    case 1680: DLLMC_R(1, 1, 5); break;
+    case 3232: DLLMC_R(1, 2, 2); break;
+    case 3248: DLLMC_R(1, 2, 3); break;
+    case 3264: DLLMC_R(1, 2, 4); break;
+    case 3280: DLLMC_R(1, 2, 5); break;
+    case 4816: DLLMC_R(1, 3, 1); break;
+    case 6416: DLLMC_R(2, 2, 1); break;
+    case 6432: DLLMC_R(2, 2, 2); break;
+    case 6448: DLLMC_R(2, 2, 3); break;
+    case 6464: DLLMC_R(2, 2, 4); break;
+    case 6480: DLLMC_R(2, 2, 5); break;
+    case 12816: DLLMC_R(2, 4, 1); break;
+    case 12864: DLLMC_R(2, 4, 4); break;
+    default: DLLMC_R(4, 2, 5); break;
   }
 #undef DLLMC_R
   if (p.S > 1) {
@@ -562,7 +570,8 @@ I8Plan plan_i8(int M, int N, int Kp) {
   for (const I8Cost& c : kI8Costs) {
     const long long mt = (M + c.bm - 1) / c.bm, nt = (N + c.bn - 1) / c.bn;
     if (mt > 65535) continue;  // (the grid's second dimension)
-    for (int S = 1; S <= (c.wide ? 1 : 8); S *= 2) {
+    for (const int S : {1, 2, 3, 4, 6, 8}) {
+      if (S > 1 && (c.wide || S > lines)) break;
       const int per = (lines + S - 1) / S, used = (lines + per - 1) / per;
       const double rounds = static_cast<double>((mt * nt * used + 255) / 256);
       const double t = c.start + rounds * (c.round + c.line * per) + mb_w * c.w + (used == 1 ? 2 * mn * c.out : used * 4 * mn * c.sums + c.add);

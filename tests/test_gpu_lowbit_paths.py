@@ -94,9 +94,14 @@ def test_weight_kernels(dtype, fmt, B, Mq, n, H_q, H_kv, d_h, keys, ranges, rows
 
 
 LINEAR = [  # M, N, K -> rows, columns, several slices, tile kernel
-    (5, 100, 700, 16, 16, 0, 0), (574, 18, 10191, 16, 32, 1, 0), (1, 8456, 394, 16, 48, 0, 0), (66, 655, 14541, 16, 64, 1, 0), (20, 1213, 129, 32, 16, 0, 0),
-    (19, 8546, 5757, 32, 48, 0, 0), (17, 2054, 10497, 32, 48, 1, 0), (1, 8197, 1, 32, 64, 0, 0), (8262, 1, 1, 64, 16, 0, 0), (4661, 2, 5279, 64, 16, 1, 0),
-    (36, 11460, 1042, 64, 48, 0, 0), (8323, 18, 1, 64, 64, 0, 0), (1194, 17, 14122, 64, 64, 1, 0), (4581, 1, 4407, 128, 48, 1, 0), (2209, 53, 9897, 128, 64, 1, 0),
+    (3, 3, 603, 16, 16, 0, 0), (3, 3, 5632, 16, 16, 1, 0), (3, 4217, 695, 16, 48, 0, 0), (3, 1673, 10471, 16, 48, 1, 0),
+    (3, 12494, 675, 16, 80, 0, 0), (3, 2121, 11110, 16, 80, 1, 0), (3, 7996, 2022, 32, 32, 0, 0), (17, 794, 8817, 32, 32, 1, 0),
+    (17, 8199, 616, 32, 48, 0, 0), (3, 1385, 9268, 32, 48, 1, 0), (3, 16369, 787, 32, 64, 0, 0), (3, 5250, 13219, 32, 64, 1, 0),
+    (20, 16549, 622, 32, 80, 0, 0), (4326, 3, 634, 48, 16, 0, 0), (710, 3, 6786, 48, 16, 1, 0), (4266, 37, 627, 64, 16, 0, 0),
+    (2026, 3, 9829, 64, 16, 1, 0), (8347, 17, 735, 64, 32, 0, 0), (2158, 17, 6265, 64, 32, 1, 0), (66, 5477, 804, 64, 48, 0, 0),
+    (1463, 34, 7095, 64, 48, 1, 0), (33, 8692, 729, 64, 64, 0, 0), (3, 2579, 12887, 64, 64, 1, 0), (18, 18773, 727, 64, 80, 0, 0),
+    (3, 6763, 16791, 64, 80, 1, 0), (8532, 35, 702, 128, 16, 0, 0), (4328, 3, 5699, 128, 16, 1, 0), (8847, 17, 9216, 128, 64, 1, 0),
+    (66, 16435, 1052, 128, 80, 0, 0), (66, 2084, 13149, 128, 80, 1, 0),
 ]
 
 
@@ -125,21 +130,18 @@ def test_linear_ring(dtype, M, N, K, rows, cols, slices, whole):
     check_linear(dtype, M, N, K)
 
 
-TILES = [(128, 64, 512, 2141), (128, 128, 33, 17256), (128, 256, 257, 16851), (192, 128, 132, 17136), (192, 256, 395, 16573), (256, 128, 194, 17888),
-         (256, 256, 797, 14214)]
+STEPS = (1, 129, 300, 500, 640, 700, 1000)  # one to eight 128-byte steps
+TILES = [(128, 64, 512, 2141, STEPS), (128, 128, 131, 8242, STEPS), (128, 256, 257, 16851, STEPS), (192, 128, 132, 17136, STEPS),
+         (192, 256, 395, 16573, STEPS), (256, 128, 50146, 65, STEPS[:2]), (256, 128, 194, 17888, STEPS[2:]), (256, 256, 797, 14214, STEPS)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols,M,N", TILES)
-def test_linear_tiles(dtype, rows, cols, M, N):
-    """Every shape at one to eight 128-byte steps: fewer and more than its rings are deep."""
-    seen = set()
-    for K in (1, 129, 300, 500, 640, 700, 1000):
-        shape, _, whole = L.plan_linear_i8(M, N, K)
-        if whole and shape == (rows, cols):
-            seen.add(K)
-            check_linear(dtype, M, N, K)
-    assert seen == {1, 129, 300, 500, 640, 700, 1000}
+@pytest.mark.parametrize("rows,cols,M,N,lengths", TILES)
+def test_linear_tiles(dtype, rows, cols, M, N, lengths):
+    """Every shape at fewer and more steps than its rings are deep."""
+    for K in lengths:
+        assert L.plan_linear_i8(M, N, K) == ((rows, cols), 1, True)
+        check_linear(dtype, M, N, K)
 
 
 def test_linear_tile_step_counts():
