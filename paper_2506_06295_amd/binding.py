@@ -557,8 +557,8 @@ def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple
     """Address of a contiguous tensor of the current device, this dtype and shape (None stays None)."""
     if t is None:
         return None
-    d = t.get_device()
-    if d < 0 or d != torch.cuda.current_device() or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+    d = t.get_device()  # (-1: host memory; a device tensor's runtime is up)
+    if d < 0 or d != torch._C._cuda_getDevice() or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise DllmcError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
     return t.data_ptr()
@@ -570,8 +570,9 @@ def _scratch_bytes(what: str, *shape: int) -> int:
     return getattr(lib(), f"dllmc_op_{what}_scratch_bytes")(*shape)
 
 
-def _scratch(nbytes: int) -> Optional[torch.Tensor]:
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+def _scratch(nbytes: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+    # (new_empty: 1.5 us, torch.empty with a device 1.7)
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 def _need_cache(name: str, fmt: str, t: torch.Tensor, cache_rows: int, H: int, d_h: int) -> int:
@@ -609,7 +610,7 @@ def op_kv4_load(dtype: str, cache: torch.Tensor, cache_rows: int, H: int, d_h: i
     M = cache_rows if rows is None else rows.numel()
     code, tdt = _DTYPES[dtype]
     at = _need_cache("cache", "kv4", cache, cache_rows, H, d_h)
-    out = torch.empty((M, H * d_h), dtype=tdt, device="cuda")
+    out = cache.new_empty((M, H * d_h), dtype=tdt)
     _check(lib().dllmc_op_kv4_load(code, at, cache_rows, H, d_h, _need("rows", rows, torch.int32, (M,)), M, out.data_ptr(),
                                    _stream_handle()), "dllmc_op_kv4_load")
     return out
@@ -622,14 +623,15 @@ def op_attention_kv4(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache
     lens int32 [B]: keys of each sequence (n if None); row_map int32 [B, n]: cache row of each (b * n + j if None; an entry
     that is no row: no such key)."""
     code, tdt = _DTYPES[dtype]
-    B, Mq = q.shape[0], q.shape[1]
+    B, Mq = q.shape[:2]
     qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
-    kp, vp = (_need_cache(name, "kv4", t, cache_rows, H_kv, d_h) for name, t in (("k_cache", k_cache), ("v_cache", v_cache)))
+    kp = _need_cache("k_cache", "kv4", k_cache, cache_rows, H_kv, d_h)
+    vp = _need_cache("v_cache", "kv4", v_cache, cache_rows, H_kv, d_h)
     lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
     out = torch.empty_like(q)
-    lse = torch.empty((B, Mq, H_q), dtype=torch.float32, device="cuda") if with_lse else None
+    lse = q.new_empty((B, Mq, H_q), dtype=torch.float32) if with_lse else None
     nbytes = _scratch_bytes("attention_kv4", code, B, Mq, n, H_q, H_kv, d_h)
-    scratch = _scratch(nbytes)
+    scratch = _scratch(nbytes, q)
     _check(lib().dllmc_op_attention_kv4(code, qp, B, Mq, kp, vp, cache_rows, rp, lp, n, H_q, H_kv, d_h, out.data_ptr(),
                                         _ptr(lse), _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_kv4")
     return (out, lse) if with_lse else out
@@ -643,16 +645,16 @@ def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache
     dtype, or "kv4".  lse: of op_attention_kv4 over the same operands, if there is one.  out: where it goes (may be acc)."""
     code, tdt = _DTYPES[dtype]
     fmt = _format(cache_format)
-    B, Mq = q.shape[0], q.shape[1]
+    B, Mq = q.shape[:2]
     qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
     kp = _need_cache("k_cache", cache_format, k_cache, cache_rows, H_kv, d_h)
     lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
     sp, ap = _need("lse", lse, torch.float32, (B, Mq, H_q)), _need("acc", acc, torch.float32, (B, n))
     if out is None:
-        out = torch.empty((B, n), dtype=torch.float32, device="cuda")
+        out = q.new_empty((B, n), dtype=torch.float32)
     op = _need("out", out, torch.float32, (B, n))
     nbytes = _scratch_bytes("attention_weights", code, fmt, B, Mq, n, H_q, H_kv, d_h)
-    scratch = _scratch(nbytes)
+    scratch = _scratch(nbytes, q)
     _check(lib().dllmc_op_attention_weights(code, fmt, qp, B, Mq, kp, cache_rows, rp, lp, n, H_q, H_kv, d_h, sp, ap, op,
                                             _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_weights")
     return out
@@ -665,9 +667,9 @@ def op_evict(acc: torch.Tensor, keep: int, cache_rows: int, first: int = 0, last
     B, n = acc.shape
     ap = _need("acc", acc, torch.float32, (B, n))
     lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
-    kept, kept_rows = (torch.empty((B, max(keep, 0)), dtype=torch.int32, device="cuda") for _ in range(2))
-    new_lens = torch.empty(B, dtype=torch.int32, device="cuda")
-    left = torch.empty((B, max(keep, 0)), dtype=torch.float32, device="cuda")
+    left = acc.new_empty((B, max(keep, 0)))
+    kept = torch.empty_like(left, dtype=torch.int32)
+    kept_rows, new_lens = torch.empty_like(kept), acc.new_empty(B, dtype=torch.int32)
     _check(lib().dllmc_op_evict(ap, B, n, lp, rp, cache_rows, keep, first, last, kept.data_ptr(), kept_rows.data_ptr(),
                                 new_lens.data_ptr(), left.data_ptr(), _stream_handle()), "dllmc_op_evict")
     return kept, kept_rows, new_lens, left
@@ -681,10 +683,10 @@ def op_compact(cache_format: str, rows: torch.Tensor, src_rows: int, H: int, d_h
     M = rows.numel()
     dst_rows = M if dst_rows is None else dst_rows
     rp = _need("rows", rows, torch.int32, rows.shape)
-    tensors = [None if t is None else _need_cache(name, cache_format, t, r, H, d_h)
-               for name, t, r in (("k_src", k_src, src_rows), ("k_dst", k_dst, dst_rows), ("v_src", v_src, src_rows),
-                                  ("v_dst", v_dst, dst_rows))]
-    _check(lib().dllmc_op_compact(_format(cache_format), rp, M, src_rows, dst_rows, H, d_h, *tensors, _stream_handle()),
+    ks, kd = _need_cache("k_src", cache_format, k_src, src_rows, H, d_h), _need_cache("k_dst", cache_format, k_dst, dst_rows, H, d_h)
+    vs = None if v_src is None else _need_cache("v_src", cache_format, v_src, src_rows, H, d_h)
+    vd = None if v_dst is None else _need_cache("v_dst", cache_format, v_dst, dst_rows, H, d_h)
+    _check(lib().dllmc_op_compact(_format(cache_format), rp, M, src_rows, dst_rows, H, d_h, ks, kd, vs, vd, _stream_handle()),
            "dllmc_op_compact")
 
 
@@ -732,8 +734,7 @@ def op_quant8(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = Non
     K = x.shape[1]
     M = x.shape[0] if row_idx is None else row_idx.numel()
     xp, rp = _need("x", x, tdt, x.shape), _need("row_idx", row_idx, torch.int32, (M,))
-    q = torch.empty((M, i8_row_bytes(K)), dtype=torch.int8, device="cuda")
-    scale = torch.empty(M, dtype=torch.float32, device="cuda")
+    q, scale = x.new_empty((M, i8_row_bytes(K)), dtype=torch.int8), x.new_empty(M, dtype=torch.float32)
     _check(lib().dllmc_op_quant8(code, xp, rp, M, K, q.data_ptr(), scale.data_ptr(), _stream_handle()), "dllmc_op_quant8")
     return q, scale
 
@@ -745,9 +746,9 @@ def op_linear_i8(dtype: str, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Te
     M, N, kp = a.shape[0], w.shape[0], i8_row_bytes(K)
     ap, wp = _need("a", a, torch.int8, (M, kp)), _need("w", w, torch.int8, (N, kp))
     sa, sw = _need("a_scale", a_scale, torch.float32, (M,)), _need("w_scale", w_scale, torch.float32, (N,))
-    out = torch.empty((M, N), dtype=tdt, device="cuda")
+    out = a.new_empty((M, N), dtype=tdt)
     nbytes = _scratch_bytes("linear_i8", M, N, K)
-    scratch = _scratch(nbytes)
+    scratch = _scratch(nbytes, out)
     _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream_handle()),
            "dllmc_op_linear_i8")
     return out
