@@ -15,39 +15,41 @@ namespace dllmc {
 namespace {
 
 // Key operand of 16 keys of a head: as loaded, and as the matrix cores take it.  at(): first element of contraction piece c, eight
-// elements (four in float32) a lane; queries are loaded in the same deal.
+// elements (four in float32) a lane; queries are read in the same deal.  A row is kCh pieces of 16 bytes, of which lane (ln, lg) wants
+// chunk(lg, i) of row ln.  Read like that from global memory, neighbouring lanes have different rows and a CU takes in 16 bytes a
+// cycle; read along the rows (load_keys16) and turned in LDS (turn_keys16), 64: 768 keys of 128 in bf16 by a CU 6.7 and 3.0 us.  A key
+// in 4 bits is 64 bytes, and turning it costs the instructions that it saves: 4608 rows x 4608 keys x 32 heads 264 us as it is, 277 turned.
 template <typename F, typename T, int D> struct KeyOperand;
 template <typename T, int D> struct KeyOperand<Kv4Tensor, T, D> {
-  static constexpr int kC = D / 32, kQ = Parts<T>::kQ;
-  struct Raw { uint32_t w[kC], s; };
+  static constexpr int kC = D / 32, kQ = Parts<T>::kQ, kCh = D / 32;
+  static constexpr bool kAlong = false;
+  struct Raw { uint4 w[(kC + 3) / 4]; uint32_t s; };
   typedef bf16x8 Frag[kC];
   typedef bf16x8 Query[kC][kQ];
   static __device__ __forceinline__ int at(int lg, int c) { return lg * (D / 4) + 8 * c; }
-  static __device__ __forceinline__ void load(const CacheView& v, int h, int row, int lg, Raw& r) {
+  static __device__ __forceinline__ const uint4* row(const CacheView& v, int h, int row) {
     // (a head's codes end below 2^24 * 128 bytes: a scalar base and a 32-bit offset)
-    const size_t head = static_cast<size_t>(h) * v.cache_rows;
-    const uint8_t* p = v.kv4.codes + head * (D / 2) + (static_cast<uint32_t>(row) * (D / 2) + lg * (D / 8));
+    return reinterpret_cast<const uint4*>(v.kv4.codes + static_cast<size_t>(h) * v.cache_rows * (D / 2) + static_cast<uint32_t>(row) * (D / 2));
+  }
+  // what does not come along the rows
+  static __device__ __forceinline__ void load(const CacheView& v, int h, int row_, int lg, Raw& r) {
     if constexpr (D == 64) {
-      const uint2 w = *reinterpret_cast<const uint2*>(p);
-      r.w[0] = w.x; r.w[1] = w.y;
+      const uint2 w = reinterpret_cast<const uint2*>(row(v, h, row_))[lg];
+      r.w[0].x = w.x; r.w[0].y = w.y;
     } else {
 #pragma unroll
-      for (int t = 0; t < D / 128; ++t) {
-        const uint4 w = reinterpret_cast<const uint4*>(p)[t];
-        r.w[4 * t] = w.x; r.w[4 * t + 1] = w.y; r.w[4 * t + 2] = w.z; r.w[4 * t + 3] = w.w;
-      }
+      for (int t = 0; t < kC / 4; ++t) r.w[t] = row(v, h, row_)[lg * (kC / 4) + t];
     }
-    const uint8_t* q = v.kv4.scales + head * (D / 32);
-    const uint32_t at = static_cast<uint32_t>(row) * (D / 32);
+    const uint8_t* q = v.kv4.scales + static_cast<size_t>(h) * v.cache_rows * (D / 32);
+    const uint32_t at = static_cast<uint32_t>(row_) * (D / 32);
     r.s = D == 64 ? q[at + lg / 2] : D == 128 ? q[at + lg] : *reinterpret_cast<const uint16_t*>(q + (at + 2 * lg));
   }
   static __device__ __forceinline__ void expand(const Raw& r, Frag& f) {
 #pragma unroll
-    for (int c = 0; c < kC; ++c) f[c] = kv4_expand(r.w[c], D == 256 ? (r.s >> (c / 4 * 8)) & 255u : r.s);
-  }
-  static __device__ __forceinline__ void query(const T* row, int lg, Query& q) {
-#pragma unroll
-    for (int c = 0; c < kC; ++c) load_query(row + at(lg, c), q[c]);
+    for (int c = 0; c < kC; ++c) {
+      const uint4 w = r.w[c / 4];
+      f[c] = kv4_expand(c % 4 == 0 ? w.x : c % 4 == 1 ? w.y : c % 4 == 2 ? w.z : w.w, D == 256 ? (r.s >> (c / 4 * 8)) & 255u : r.s);
+    }
   }
   template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
 #pragma unroll
@@ -66,23 +68,20 @@ template <typename T, int D> struct KeyOperand<Kv4Tensor, T, D> {
   }
 };
 template <int D> struct KeyOperand<bf16_t, bf16_t, D> {
-  static constexpr int kC = D / 32;
-  struct Raw { bf16x8 w[kC]; };
+  static constexpr int kC = D / 32, kCh = 4 * kC;
+  static constexpr bool kAlong = true;
+  struct Raw { uint4 w[kC]; };
   typedef bf16x8 Frag[kC];
   typedef bf16x8 Query[kC];
   static __device__ __forceinline__ int at(int lg, int c) { return 32 * c + 8 * lg; }
-  static __device__ __forceinline__ void load(const CacheView& v, int h, int row, int lg, Raw& r) {
-    const bf16_t* p = static_cast<const bf16_t*>(v.rows) + (static_cast<size_t>(row) * v.H + h) * D;
-#pragma unroll
-    for (int c = 0; c < kC; ++c) r.w[c] = *reinterpret_cast<const bf16x8*>(p + at(lg, c));
+  static __device__ __forceinline__ int chunk(int lg, int i) { return 4 * i + lg; }
+  static __device__ __forceinline__ const uint4* row(const CacheView& v, int h, int row) {
+    return reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(v.rows) + (static_cast<size_t>(row) * v.H + h) * D);
   }
+  static __device__ __forceinline__ void load(const CacheView&, int, int, int, Raw&) {}
   static __device__ __forceinline__ void expand(const Raw& r, Frag& f) {
 #pragma unroll
-    for (int c = 0; c < kC; ++c) f[c] = r.w[c];
-  }
-  static __device__ __forceinline__ void query(const bf16_t* row, int lg, Query& q) {
-#pragma unroll
-    for (int c = 0; c < kC; ++c) q[c] = *reinterpret_cast<const bf16x8*>(row + at(lg, c));
+    for (int c = 0; c < kC; ++c) f[c] = __builtin_bit_cast(bf16x8, r.w[c]);
   }
   template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
 #pragma unroll
@@ -96,23 +95,20 @@ template <int D> struct KeyOperand<bf16_t, bf16_t, D> {
   }
 };
 template <int D> struct KeyOperand<float, float, D> {
-  static constexpr int kC = D / 16;
-  struct Raw { f32x4 w[kC]; };
+  static constexpr int kC = D / 16, kCh = 4 * kC;
+  static constexpr bool kAlong = true;
+  struct Raw { uint4 w[kC]; };
   typedef f32x4 Frag[kC];
   typedef f32x4 Query[kC];
   static __device__ __forceinline__ int at(int lg, int c) { return 16 * c + 4 * lg; }
-  static __device__ __forceinline__ void load(const CacheView& v, int h, int row, int lg, Raw& r) {
-    const float* p = static_cast<const float*>(v.rows) + (static_cast<size_t>(row) * v.H + h) * D;
-#pragma unroll
-    for (int c = 0; c < kC; ++c) r.w[c] = *reinterpret_cast<const f32x4*>(p + at(lg, c));
+  static __device__ __forceinline__ int chunk(int lg, int i) { return 4 * i + lg; }
+  static __device__ __forceinline__ const uint4* row(const CacheView& v, int h, int row) {
+    return reinterpret_cast<const uint4*>(static_cast<const float*>(v.rows) + (static_cast<size_t>(row) * v.H + h) * D);
   }
+  static __device__ __forceinline__ void load(const CacheView&, int, int, int, Raw&) {}
   static __device__ __forceinline__ void expand(const Raw& r, Frag& f) {
 #pragma unroll
-    for (int c = 0; c < kC; ++c) f[c] = r.w[c];
-  }
-  static __device__ __forceinline__ void query(const float* row, int lg, Query& q) {
-#pragma unroll
-    for (int c = 0; c < kC; ++c) q[c] = *reinterpret_cast<const f32x4*>(row + at(lg, c));
+    for (int c = 0; c < kC; ++c) f[c] = __builtin_bit_cast(f32x4, r.w[c]);
   }
   template <typename P> static __device__ __forceinline__ void query_pieces(P&& piece, int lg, Query& q) {
 #pragma unroll
@@ -136,9 +132,88 @@ __device__ __forceinline__ size_t row_of(const WeighShape& s, int b, int h, int 
   return (static_cast<size_t>(b) * s.Mq + i) * s.H_q + h * s.G + (r - i * s.G);
 }
 
+// Cache rows of the N keys key0, key0 + 16, .., negative where there is none.  (the lookups are made for keys in range whether they
+// are there or not: none waits for a branch)
+template <int N> __device__ __forceinline__ void key_rows(const Keys& keys, int b, int key0, int len, int (&r)[N]) {
+  int at[N];
+#pragma unroll
+  for (int t = 0; t < N; ++t) at[t] = min(key0 + t * 16, keys.n - 1);
+  if (keys.row_map != nullptr) {
+    const int* map = keys.row_map + static_cast<size_t>(b) * keys.n;
+#pragma unroll
+    for (int t = 0; t < N; ++t) r[t] = map[at[t]];
+  } else {
+#pragma unroll
+    for (int t = 0; t < N; ++t) r[t] = b * keys.n + at[t];
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+    if (key0 + t * 16 >= len || static_cast<unsigned>(r[t]) >= static_cast<unsigned>(keys.cache_rows)) r[t] = -1;
+}
+
+// ROWS query rows for all NW wavefronts of a workgroup, loaded along the rows into LDS (in a fragment's order by every wavefront for itself,
+// 64 rows of 128 in bf16 by eight of them would keep a CU's address unit for 3.9 us).
+template <typename T, int D, int ROWS, int NW> struct QueryTile {
+  static constexpr int kCh = D * static_cast<int>(sizeof(T)) / 16, kMix = kCh < 16 ? kCh : 16, kVecs = ROWS * kCh;
+  // row(r): address of row r.  Wait for the loads and for each other before piece().
+  template <typename Row> static __device__ __forceinline__ void issue(Row&& row, uint4* lds, int wave, int lane) {
+#pragma unroll
+    for (int j = 0; j < (kVecs / 64 + NW - 1) / NW; ++j) {
+      const int i = wave + j * NW;
+      if (i >= kVecs / 64) break;
+      const int v = i * 64 + lane, r = v / kCh, c = (v % kCh) ^ (r % kMix);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(row(r)) + c, &lds[i * 64], 16, 0, 0);
+    }
+  }
+  // 16 bytes c of row r
+  static __device__ __forceinline__ uint4 piece(const uint4* lds, int r, int c) { return lds[r * kCh + (c ^ (r % kMix))]; }
+};
+
+constexpr float kLowest = -3.4028234663852886e38f;
+
+// 16 keys of a head; lane ln (and ln + 16, ..) names the cache row of key ln
+template <typename Op> struct KeyTurn {
+  static constexpr int kWide = Op::kCh < 32 ? Op::kCh : 32, kVecs = Op::kAlong ? 16 * kWide : 0;  // a wavefront's 16-byte slots of LDS
+  static __device__ __forceinline__ int mix(int r) { return r % (kWide < 16 ? kWide : 16); }
+};
+template <typename Op> __device__ __forceinline__ void load_keys16(const CacheView& v, int h, int row, int lane, typename Op::Raw& raw) {
+  constexpr int W = KeyTurn<Op>::kWide;
+  if constexpr (Op::kAlong) {
+#pragma unroll
+    for (int u = 0; u < Op::kCh / W; ++u)
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const int x = i * 64 + lane;
+        raw.w[u * (W / 4) + i] = Op::row(v, h, __shfl(row, x / W, 64))[u * W + x % W];
+      }
+  }
+  Op::load(v, h, row, lane / 16, raw);
+}
+// (`lds` is the wavefront's own, and the LDS keeps a wavefront's order by itself)
+template <typename Op> __device__ __forceinline__ void turn_keys16(typename Op::Raw& raw, uint4* lds, int lane) {
+  typedef KeyTurn<Op> K;
+  constexpr int W = K::kWide;
+  if constexpr (Op::kAlong) {
+#pragma unroll
+    for (int u = 0; u < Op::kCh / W; ++u) {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const int x = i * 64 + lane, r = x / W;
+        lds[r * W + ((x % W) ^ K::mix(r))] = raw.w[u * (W / 4) + i];
+      }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i)
+        raw.w[u * (W / 4) + i] = lds[lane % 16 * W + ((Op::chunk(lane / 16, u * (W / 4) + i) - u * W) ^ K::mix(lane % 16))];
+      asm volatile("" ::: "memory");
+    }
+  }
+}
+
 // (m, l) of 16 QB rows over a range of keys, base 2, or m and 1 / l where the range is all of them; the eight wavefronts deal the range's blocks
-// of 32 keys, the next one in flight.  Bound by vector instructions (one per 5 cycles: 4.5 a score) and the products
-// beside them: 0.66 of what the products alone would take, 4608 rows x 4608 keys x 32 heads.
+// of 32 keys, the next one in flight.  Bound by vector instructions: 4.6 a score, one per 6 cycles with two wavefronts per SIMD (an
+// exponential 12); with four of them, queries read from LDS again for every block, the same.  512 rows x 4608 keys x 32 heads in 4 bits
+// 33 us, 4608 rows 264, of which the products alone would take 129.
 constexpr int kSW = 8;
 template <typename F, typename T, int D, int QB>
 __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_stats(const T* __restrict__ q, WeighShape s, CacheView k,
@@ -146,7 +221,9 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
                                                                                             float* __restrict__ m_out,
                                                                                             float* __restrict__ il_out) {
   typedef KeyOperand<F, T, D> Op;
+  typedef QueryTile<T, D, 16 * QB, kSW> Rows;
   __shared__ float2 hand[kSW][16 * QB];
+  __shared__ __attribute__((aligned(1024))) uint4 lds[Rows::kVecs + kSW * KeyTurn<Op>::kVecs];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
   int x = xcd_group_item(blockIdx.x, gridDim.x, s.tiles);  // tiles of one head and range read the same keys
@@ -157,30 +234,37 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
   const int nblk = (len + 31) / 32, blk1 = min(nblk, (range + 1) * s.per);
   int blk = range * s.per + wave;
   const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
-  float m[QB], l[QB];
+  float m[QB], ref[QB], l[QB];  // l: sum of exp2(sl2e s - ref)
 #pragma unroll
-  for (int i = 0; i < QB; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+  for (int i = 0; i < QB; ++i) { m[i] = -INFINITY; ref[i] = kLowest; l[i] = 0.f; }
   struct Block { typename Op::Raw k[2]; uint32_t there; };
-  auto rows_of = [&](int blk_, int (&r)[2]) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int j = blk_ * 32 + t * 16 + ln;
-      r[t] = j < len ? keys.row(b, j) : -1;
-    }
-  };
+  auto rows_of = [&](int blk_, int (&r)[2]) { key_rows(keys, b, blk_ * 32 + ln, len, r); };
   auto fetch = [&](const int (&r)[2], Block& kb) {
     kb.there = static_cast<uint32_t>(__ballot(r[0] >= 0) & 0xffffu) | static_cast<uint32_t>(__ballot(r[1] >= 0) & 0xffffu) << 16;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) Op::load(k, h, max(r[t], 0), lg, kb.k[t]);
+    for (int t = 0; t < 2; ++t) load_keys16<Op>(k, h, max(r[t], 0), lane, kb.k[t]);
   };
+  Rows::issue([&](int r) { return q + row_of(s, b, h, min(r0 + r, s.NR - 1)) * D; }, lds, wave, lane);
+  Block b0, b1;
+  int r[2];
+  if (blk < blk1) {
+    rows_of(blk, r);
+    fetch(r, b0);
+    rows_of(min(blk + kSW, blk1 - 1), r);
+  }
+  wait_vmcnt_lds<0>();
+  __syncthreads();
   if (blk < blk1) {
     typename Op::Query qf[QB];
-    auto use = [&](const Block& kb) {
+#pragma unroll
+    for (int i = 0; i < QB; ++i) Op::query_pieces([&](int c) { return Rows::piece(lds, i * 16 + ln, c); }, lg, qf[i]);
+    auto use = [&](Block& kb) {
       if (kb.there == 0) return;
       f32x4 st[2][QB];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         typename Op::Frag f;
+        turn_keys16<Op>(kb.k[t], lds + Rows::kVecs + wave * KeyTurn<Op>::kVecs, lane);
         Op::expand(kb.k[t], f);
 #pragma unroll
         for (int i = 0; i < QB; ++i) st[t][i] = Op::scores(f, qf[i]);
@@ -198,28 +282,30 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
       // (every lane has a maximum and sum of its own quarter of the keys, joined at the end)
 #pragma unroll
       for (int i = 0; i < QB; ++i) {
-        float mx = st[0][i][0];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[t][i][e]);
-        const float top = fmaxf(m[i], mx * sl2e), u = top == -INFINITY ? 0.f : top;
-        float sum = l[i] * __builtin_amdgcn_exp2f(m[i] - u);
+          for (int e = 0; e < 4; ++e) m[i] = fmaxf(m[i], st[t][i][e]);
+        const float u = fmaxf(m[i] * sl2e, kLowest);  // finite: no key, no NaN
+        float sum = l[i] * __builtin_amdgcn_exp2f(ref[i] - u);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(st[t][i][e], sl2e, -u));
         l[i] = sum;
-        m[i] = top;
+        ref[i] = u;
       }
     };
-    Block b0, b1;
-    int r[2];
-    rows_of(blk, r);
-    fetch(r, b0);
-    rows_of(min(blk + kSW, blk1 - 1), r);
-#pragma unroll
-    for (int i = 0; i < QB; ++i) Op::query(q + row_of(s, b, h, min(r0 + i * 16 + ln, s.NR - 1)) * D, lg, qf[i]);
+    if constexpr (sizeof(typename Op::Raw) >= 256) {  // (two of them do not fit in the registers)
+      while (true) {
+        use(b0);
+        blk += kSW;
+        if (blk >= blk1) break;
+        fetch(r, b0);
+        rows_of(min(blk + kSW, blk1 - 1), r);
+      }
+      blk = blk1;
+    }
     for (; blk + kSW < blk1; blk += 2 * kSW) {
       fetch(r, b1);
       rows_of(min(blk + 2 * kSW, blk1 - 1), r);
@@ -237,7 +323,7 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
   };
 #pragma unroll
   for (int i = 0; i < QB; ++i) {
-    float2 v = make_float2(m[i], l[i]);
+    float2 v = make_float2(m[i] * sl2e, l[i]);
     v = join(v, make_float2(__shfl_xor(v.x, 16, 64), __shfl_xor(v.y, 16, 64)));
     v = join(v, make_float2(__shfl_xor(v.x, 32, 64), __shfl_xor(v.y, 32, 64)));
     if (lg == 0) hand[wave][i * 16 + ln] = v;
@@ -287,19 +373,22 @@ __device__ __forceinline__ void store_columns(f32x4 (&sum)[KB], const uint32_t (
   }
 }
 template <typename Op, int KB>
-__device__ __forceinline__ void load_keys(const CacheView& k, const Keys& keys, int b, int h, int key0, int len, int ln, int lg,
+__device__ __forceinline__ void load_keys(const CacheView& k, const Keys& keys, int b, int h, int key0, int len, int lane, uint4* lds,
                                           typename Op::Frag (&f)[KB], uint32_t (&there)[KB]) {
+  const int ln = lane % 16;
   int r[KB];
   typename Op::Raw raw[KB];
-#pragma unroll
-  for (int t = 0; t < KB; ++t) r[t] = key0 + t * 16 + ln < len ? keys.row(b, key0 + t * 16 + ln) : -1;
+  key_rows(keys, b, key0 + ln, len, r);
 #pragma unroll
   for (int t = 0; t < KB; ++t) {
     there[t] = static_cast<uint32_t>(__ballot(r[t] >= 0));  // (lanes 0 .. 15: the keys)
-    Op::load(k, h, max(r[t], 0), lg, raw[t]);  // what is not there: row 0, counts for nothing
+    load_keys16<Op>(k, h, max(r[t], 0), lane, raw[t]);  // what is not there: row 0, counts for nothing
   }
 #pragma unroll
-  for (int t = 0; t < KB; ++t) Op::expand(raw[t], f[t]);
+  for (int t = 0; t < KB; ++t) {
+    turn_keys16<Op>(raw[t], lds, lane);
+    Op::expand(raw[t], f[t]);
+  }
 }
 
 // Column sums: a wavefront holds 16 KB keys of one KV head and walks its share of the head's rows; rows come in stages of 8 KB (16
@@ -317,7 +406,7 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
   typedef WeighStage<T, D> St;
   constexpr int kIssued = St::kLoads + 2;
   constexpr int NS = St::kStages, kChunks = St::kRow / 16, kMix = kChunks < 16 ? kChunks : 16;
-  __shared__ __attribute__((aligned(1024))) uint4 lds[NS * St::kVecs + NS * 4 * 32];
+  __shared__ __attribute__((aligned(1024))) uint4 lds[NS * St::kVecs + NS * 4 * 32 + 4 * KeyTurn<Op>::kVecs];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
   int x = xcd_group_item(blockIdx.x, gridDim.x, s.blocks);  // key blocks of one head and share read the same rows
@@ -351,7 +440,7 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
   typename Op::Frag kf[KB];
 #pragma unroll
   for (int t = 0; t < KB; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  load_keys<Op, KB>(k, keys, b, h, key0, len, ln, lg, kf, there);
+  load_keys<Op, KB>(k, keys, b, h, key0, len, lane, lds + NS * (St::kVecs + 4 * 32) + wave * KeyTurn<Op>::kVecs, kf, there);
   const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
   int slot = 0;
   for (int t = t0; t < t1; ++t) {
@@ -397,7 +486,9 @@ template <typename F, typename T, int D, int KB>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_short(const T* __restrict__ q, WeighShape s, CacheView k,
                                                                                          Keys keys, float* __restrict__ part) {
   typedef KeyOperand<F, T, D> Op;
+  typedef QueryTile<T, D, 16, 8> Rows;
   __shared__ float2 ml[2][8][16];
+  __shared__ __attribute__((aligned(1024))) uint4 lds[2 * Rows::kVecs + 8 * KeyTurn<Op>::kVecs];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 16, lg = lane / 16;
   int x = xcd_group_item(blockIdx.x, gridDim.x, s.RS);  // shares of one head read the same keys
@@ -410,41 +501,55 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   typename Op::Frag kf[KB];
   typename Op::Query qf;
   const int t0 = share * s.share, t1 = min((s.NR + 15) / 16, t0 + s.share);
-  auto fetch = [&](int t) { Op::query(q + row_of(s, b, h, min(t * 16 + ln, s.NR - 1)) * D, lg, qf); };
-  fetch(t0);
+  auto issue = [&](int t) {
+    Rows::issue([&](int r) { return q + row_of(s, b, h, min(t * 16 + r, s.NR - 1)) * D; }, lds + (t & 1) * Rows::kVecs, wave, lane);
+  };
+  issue(t0);
 #pragma unroll
   for (int t = 0; t < KB; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  load_keys<Op, KB>(k, keys, b, h, key0, len, ln, lg, kf, there);
+  load_keys<Op, KB>(k, keys, b, h, key0, len, lane, lds + 2 * Rows::kVecs + wave * KeyTurn<Op>::kVecs, kf, there);
   uint32_t mine = 0;  // bit 4 t + e: this lane's key e of the 16 t-th is there
 #pragma unroll
   for (int t = 0; t < KB; ++t) mine |= ((there[t] >> (4 * lg)) & 15u) << (4 * t);
+  bool all = true;  // wavefront-uniform
+#pragma unroll
+  for (int t = 0; t < KB; ++t) all &= (there[t] & 0xffffu) == 0xffffu;
   const float sl2e = kLog2e / sqrtf(static_cast<float>(D));
+  wait_vmcnt_lds<0>();
+  __syncthreads();
   for (int t = t0; t < t1; ++t) {
+    if (t + 1 < t1) issue(t + 1);  // (all have read tile t - 1: they have met since)
+    Op::query_pieces([&](int c) { return Rows::piece(lds + (t & 1) * Rows::kVecs, ln, c); }, lg, qf);
     f32x4 st[KB];
     float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int u = 0; u < KB; ++u) st[u] = Op::scores(kf[u], qf);
-    if (t + 1 < t1) fetch(t + 1);
+    if (!all) {
+#pragma unroll
+      for (int u = 0; u < KB; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (((mine >> (4 * u + e)) & 1) == 0) st[u][e] = -INFINITY;
+    }
 #pragma unroll
     for (int u = 0; u < KB; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        st[u][e] = (mine >> (4 * u + e)) & 1 ? st[u][e] * sl2e : -INFINITY;
-        m = fmaxf(m, st[u][e]);
-      }
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, st[u][e]);
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
+    m *= sl2e;
     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int u = 0; u < KB; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        st[u][e] = __builtin_amdgcn_exp2f(st[u][e] - ref);
+        st[u][e] = __builtin_amdgcn_exp2f(fmaf(st[u][e], sl2e, -ref));
         l += st[u][e];
       }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (lg == 0) ml[t & 1][wave][ln] = make_float2(m, l);
+    wait_vmcnt_lds<0>();
     __syncthreads();
     float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -454,14 +559,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       const float2 c = ml[t & 1][w][ln];
       L += c.y != c.y ? c.y : c.x == -INFINITY ? 0.f : c.y * __builtin_amdgcn_exp2f(c.x - M);
     }
-    // what this wavefront's exponentials are short of; nothing for rows past the last one and wavefronts without keys
+    // what this wavefront's exponentials are short of; nothing for rows past the last one (they repeat it: where they are NaN, so is it)
+    // and wavefronts without keys
     float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;
     if (L != L) f = L;
     if (t * 16 + ln >= s.NR) f = 0.f;
 #pragma unroll
     for (int u = 0; u < KB; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[u][e] += (t * 16 + ln >= s.NR) ? 0.f : st[u][e] * f;
+      for (int e = 0; e < 4; ++e) sum[u][e] = fmaf(st[u][e], f, sum[u][e]);
   }
   if (key0 < keys.n)
     store_columns<KB>(sum, there, key0, keys.n, ln, lg, part + (static_cast<size_t>(share * B + b) * s.H_kv + h) * keys.n);
