@@ -418,23 +418,42 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
   float* out = part + (static_cast<size_t>(share * B + b) * s.H_kv + h) * keys.n;
   const int t0 = share * s.share, t1 = min((s.NR + St::kRows - 1) / St::kRows, t0 + s.share);
 
-  // loader: instruction j of a stage copies 1 KB, wavefront w issues kLoads w .. + kLoads - 1 and its own copy of m and 1 / l
+  // loader: instruction j of a stage copies 1 KB, wavefront w issues kLoads w .. + kLoads - 1 and its own copy of m and 1 / l.  Rows
+  // are walked, not computed: at[] is the row of q (of this sequence) of the next stage, g[] its head in the group, a stage further
+  // is kRows / G queries and kRows % G heads (rows past the last one: the last one)
   const float* second = il != nullptr ? il : m;
-  auto issue = [&](int slot, int t) {
+  const size_t seq = static_cast<size_t>(b) * s.Mq * s.H_q;
+  const T* qb = q + seq * D;
+  const float *mb = m + seq, *sb = second + seq;
+  const int over = St::kRows % s.G, step = St::kRows / s.G * s.H_q + over, last = (s.Mq - 1) * s.H_q + h * s.G + s.G - 1;
+  int at[St::kLoads + 1], g[St::kLoads + 1];
+#pragma unroll
+  for (int j = 0; j <= St::kLoads; ++j) {
+    const int r = t0 * St::kRows + (j < St::kLoads ? ((wave * St::kLoads + j) * 64 + lane) / kChunks : lane % St::kRows);
+    g[j] = r % s.G;
+    at[j] = r / s.G * s.H_q + h * s.G + g[j];
+  }
+  auto issue = [&](int slot) {
 #pragma unroll
     for (int j = 0; j < St::kLoads; ++j) {
-      const int v = (wave * St::kLoads + j) * 64 + lane, r = v / kChunks, c = (v % kChunks) ^ (r % kMix);
-      const size_t w = row_of(s, b, h, min(t * St::kRows + r, s.NR - 1));
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(q + w * D) + c, &lds[slot * St::kVecs + (wave * St::kLoads + j) * 64],
-                                       16, 0, 0);
+      const int v = (wave * St::kLoads + j) * 64 + lane, c = (v % kChunks) ^ (v / kChunks % kMix);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(qb) + (static_cast<size_t>(min(at[j], last)) * kChunks + c),
+                                       &lds[slot * St::kVecs + (wave * St::kLoads + j) * 64], 16, 0, 0);
     }
-    const size_t w = row_of(s, b, h, min(t * St::kRows + lane % St::kRows, s.NR - 1));
-    __builtin_amdgcn_global_load_lds(m + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32], 4, 0, 0);
-    __builtin_amdgcn_global_load_lds(second + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32 + 16], 4, 0, 0);
+    const int w = min(at[St::kLoads], last);
+    __builtin_amdgcn_global_load_lds(mb + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32], 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(sb + w, &lds[NS * St::kVecs + (slot * 4 + wave) * 32 + 16], 4, 0, 0);
+#pragma unroll
+    for (int j = 0; j <= St::kLoads; ++j) {
+      const int next = g[j] + over;
+      const bool wrap = next >= s.G;
+      g[j] = wrap ? next - s.G : next;
+      at[j] += wrap ? step + s.H_q - s.G : step;
+    }
   };
 #pragma unroll
   for (int t = 0; t < NS - 1; ++t)
-    if (t0 + t < t1) issue(t, t0 + t);
+    if (t0 + t < t1) issue(t);
   f32x4 sum[KB];
   uint32_t there[KB];
   typename Op::Frag kf[KB];
@@ -449,7 +468,7 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
     else if (rem == 1) wait_vmcnt_lds<kIssued>();
     else wait_vmcnt_lds<0>();
     __builtin_amdgcn_s_barrier();  // stage t is there for everybody, and everybody has read stage t - 1, which is filled next
-    if (t + NS - 1 < t1) issue(slot == 0 ? NS - 1 : slot - 1, t + NS - 1);
+    if (t + NS - 1 < t1) issue(slot == 0 ? NS - 1 : slot - 1);
     if (key0 < len) {
 #pragma unroll
       for (int g = 0; g < St::kRows / 16; ++g) {
