@@ -187,14 +187,10 @@ __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const A
     bool moved = false;
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
-      float mx = -INFINITY;
+      float mx = fmaxf(fmaxf(st[0][i][0], st[0][i][1]), st[0][i][2]);
 #pragma unroll
-      for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[sb][i][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mb = mx * sl2e;
+      for (int x = 3; x < 8; ++x) mx = fmaxf(mx, st[x / 4][i][x % 4]);
+      const float mb = groups_max(mx) * sl2e;
       m_new[i] = mb > m_run[i] + kLazyMax ? mb : m_run[i];
       m_use[i] = m_new[i] == -INFINITY ? 0.f : m_new[i];
       moved |= m_new[i] != m_run[i];
@@ -491,8 +487,14 @@ __device__ __forceinline__ void attend_tile_body(const bf16_t* __restrict__ q, c
         for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[sb][i][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        // (heads of 128: the exchange competes with the products' neighbours, 4608 rows x 4608 keys x 32 heads 448 us through LDS, 454 without;
+        // of 64, 512 rows x 2048 keys x 8 heads 10.6 and 10.3)
+        if (D == 64) {
+          mx = groups_max(mx);
+        } else {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        }
         const float mb = mx * sl2e;
         m_new[i] = mb > m_run[i] + kLazyMax ? mb : m_run[i];
         m_use[i] = m_new[i] == -INFINITY ? 0.f : m_new[i];

@@ -554,9 +554,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int u = 0; u < KB; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = fmaxf(m, st[u][e]);
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-    m *= sl2e;
+    m = groups_max(m) * sl2e;
     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int u = 0; u < KB; ++u)
@@ -565,8 +563,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         st[u][e] = __builtin_amdgcn_exp2f(fmaf(st[u][e], sl2e, -ref));
         l += st[u][e];
       }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    l = groups_sum(l);
     if (lg == 0) ml[t & 1][wave][ln] = make_float2(m, l);
     wait_vmcnt_lds<0>();
     __syncthreads();

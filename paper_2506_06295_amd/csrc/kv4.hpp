@@ -59,6 +59,22 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false));  // (lane 15 - l of the 16)
 }
 
+// Maximum and sum over lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them: two exchanges of rows of lanes between registers, no trip through LDS.
+template <typename F> __device__ __forceinline__ float over_groups(float v, F&& f) {
+  typedef uint32_t pair_t __attribute__((ext_vector_type(2)));
+  uint32_t u = __float_as_uint(v);
+  const pair_t a = __builtin_bit_cast(pair_t, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+  u = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const pair_t b = __builtin_bit_cast(pair_t, __builtin_amdgcn_permlane32_swap(u, u, false, false));
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float groups_max(float v) {
+  return over_groups(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float groups_sum(float v) {
+  return over_groups(v, [](float a, float b) { return a + b; });
+}
+
 // Scale byte of a block whose largest magnitude has the bits `top`: 127 + the smallest e with top <= 6 * 2^e = 1.5 * 2^(e + 2), so
 // that nothing saturates; at least 2 (no value below 2^-126), at most 252 (6 * 2^125 is finite: above it values do saturate).
 __device__ __forceinline__ uint32_t kv4_scale_byte(uint32_t top) {
