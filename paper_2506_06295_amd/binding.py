@@ -234,6 +234,10 @@ def _stream_handle() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -553,12 +557,19 @@ def op_attention(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
 
 
 # ---- the step's pieces in fewer bits ------------------------------------------------------------
-def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple) -> Optional[int]:
-    """Address of a contiguous tensor of the current device, this dtype and shape (None stays None)."""
+def _device(name: str, t: torch.Tensor) -> int:
+    """Index of the current device, which t has to be on."""
+    d = t.get_device()  # (-1: host memory; a device tensor's runtime is up)
+    if d < 0 or d != torch._C._cuda_getDevice():
+        raise DllmcError(f"{name}: need a tensor on the current device, got one on {t.device}")
+    return d
+
+
+def _need(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: int) -> Optional[int]:
+    """Address of a contiguous tensor of this device, dtype and shape (None stays None)."""
     if t is None:
         return None
-    d = t.get_device()  # (-1: host memory; a device tensor's runtime is up)
-    if d < 0 or d != torch._C._cuda_getDevice() or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise DllmcError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
     return t.data_ptr()
@@ -575,10 +586,10 @@ def _scratch(nbytes: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
-def _need_cache(name: str, fmt: str, t: torch.Tensor, cache_rows: int, H: int, d_h: int) -> int:
+def _need_cache(name: str, fmt: str, t: torch.Tensor, cache_rows: int, H: int, d_h: int, device: int) -> int:
     if fmt == "kv4":
-        return _need(name, t, torch.uint8, (kv4_bytes(cache_rows, H, d_h),))
-    return _need(name, t, _DTYPES[fmt][1], (cache_rows, H * d_h))
+        return _need(name, t, torch.uint8, (kv4_bytes(cache_rows, H, d_h),), device)
+    return _need(name, t, _DTYPES[fmt][1], (cache_rows, H * d_h), device)
 
 
 def _format(fmt: str) -> int:
@@ -599,9 +610,10 @@ def op_kv4_store(dtype: str, x: torch.Tensor, cache: torch.Tensor, cache_rows: i
     """Rows of x [M, H * d_h] into rows `rows` (int32 [M], distinct; 0 .. M - 1 if None) of a 4-bit cache tensor."""
     M = x.shape[0]
     code, tdt = _DTYPES[dtype]
-    _check(lib().dllmc_op_kv4_store(code, _need("x", x, tdt, (M, H * d_h)), M, _need("rows", rows, torch.int32, (M,)),
-                                    _need_cache("cache", "kv4", cache, cache_rows, H, d_h), cache_rows, H, d_h,
-                                    _stream_handle()), "dllmc_op_kv4_store")
+    dev = _device("x", x)
+    _check(lib().dllmc_op_kv4_store(code, _need("x", x, tdt, (M, H * d_h), dev), M, _need("rows", rows, torch.int32, (M,), dev),
+                                    _need_cache("cache", "kv4", cache, cache_rows, H, d_h, dev), cache_rows, H, d_h,
+                                    _stream(dev)), "dllmc_op_kv4_store")
 
 
 def op_kv4_load(dtype: str, cache: torch.Tensor, cache_rows: int, H: int, d_h: int,
@@ -609,10 +621,11 @@ def op_kv4_load(dtype: str, cache: torch.Tensor, cache_rows: int, H: int, d_h: i
     """[M, H * d_h]: the values of rows `rows` (int32 [M]; all if None) of a 4-bit cache tensor."""
     M = cache_rows if rows is None else rows.numel()
     code, tdt = _DTYPES[dtype]
-    at = _need_cache("cache", "kv4", cache, cache_rows, H, d_h)
+    dev = _device("cache", cache)
+    at = _need_cache("cache", "kv4", cache, cache_rows, H, d_h, dev)
     out = cache.new_empty((M, H * d_h), dtype=tdt)
-    _check(lib().dllmc_op_kv4_load(code, at, cache_rows, H, d_h, _need("rows", rows, torch.int32, (M,)), M, out.data_ptr(),
-                                   _stream_handle()), "dllmc_op_kv4_load")
+    _check(lib().dllmc_op_kv4_load(code, at, cache_rows, H, d_h, _need("rows", rows, torch.int32, (M,), dev), M, out.data_ptr(),
+                                   _stream(dev)), "dllmc_op_kv4_load")
     return out
 
 
@@ -624,16 +637,17 @@ def op_attention_kv4(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache
     that is no row: no such key)."""
     code, tdt = _DTYPES[dtype]
     B, Mq = q.shape[:2]
-    qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
-    kp = _need_cache("k_cache", "kv4", k_cache, cache_rows, H_kv, d_h)
-    vp = _need_cache("v_cache", "kv4", v_cache, cache_rows, H_kv, d_h)
-    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
+    dev = _device("q", q)
+    qp = _need("q", q, tdt, (B, Mq, H_q * d_h), dev)
+    kp = _need_cache("k_cache", "kv4", k_cache, cache_rows, H_kv, d_h, dev)
+    vp = _need_cache("v_cache", "kv4", v_cache, cache_rows, H_kv, d_h, dev)
+    lp, rp = _need("lens", lens, torch.int32, (B,), dev), _need("row_map", row_map, torch.int32, (B, n), dev)
     out = torch.empty_like(q)
     lse = q.new_empty((B, Mq, H_q), dtype=torch.float32) if with_lse else None
     nbytes = _scratch_bytes("attention_kv4", code, B, Mq, n, H_q, H_kv, d_h)
     scratch = _scratch(nbytes, q)
     _check(lib().dllmc_op_attention_kv4(code, qp, B, Mq, kp, vp, cache_rows, rp, lp, n, H_q, H_kv, d_h, out.data_ptr(),
-                                        _ptr(lse), _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_kv4")
+                                        _ptr(lse), _ptr(scratch), nbytes, _stream(dev)), "dllmc_op_attention_kv4")
     return (out, lse) if with_lse else out
 
 
@@ -646,17 +660,18 @@ def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache
     code, tdt = _DTYPES[dtype]
     fmt = _format(cache_format)
     B, Mq = q.shape[:2]
-    qp = _need("q", q, tdt, (B, Mq, H_q * d_h))
-    kp = _need_cache("k_cache", cache_format, k_cache, cache_rows, H_kv, d_h)
-    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
-    sp, ap = _need("lse", lse, torch.float32, (B, Mq, H_q)), _need("acc", acc, torch.float32, (B, n))
+    dev = _device("q", q)
+    qp = _need("q", q, tdt, (B, Mq, H_q * d_h), dev)
+    kp = _need_cache("k_cache", cache_format, k_cache, cache_rows, H_kv, d_h, dev)
+    lp, rp = _need("lens", lens, torch.int32, (B,), dev), _need("row_map", row_map, torch.int32, (B, n), dev)
+    sp, ap = _need("lse", lse, torch.float32, (B, Mq, H_q), dev), _need("acc", acc, torch.float32, (B, n), dev)
     if out is None:
         out = q.new_empty((B, n), dtype=torch.float32)
-    op = _need("out", out, torch.float32, (B, n))
+    op = _need("out", out, torch.float32, (B, n), dev)
     nbytes = _scratch_bytes("attention_weights", code, fmt, B, Mq, n, H_q, H_kv, d_h)
     scratch = _scratch(nbytes, q)
     _check(lib().dllmc_op_attention_weights(code, fmt, qp, B, Mq, kp, cache_rows, rp, lp, n, H_q, H_kv, d_h, sp, ap, op,
-                                            _ptr(scratch), nbytes, _stream_handle()), "dllmc_op_attention_weights")
+                                            _ptr(scratch), nbytes, _stream(dev)), "dllmc_op_attention_weights")
     return out
 
 
@@ -665,13 +680,14 @@ def op_evict(acc: torch.Tensor, keep: int, cache_rows: int, first: int = 0, last
     """(kept [B, keep], kept_rows [B, keep], new_lens [B] int32, acc [B, keep] float32): the positions that stay, see
     dllmc_op_evict."""
     B, n = acc.shape
-    ap = _need("acc", acc, torch.float32, (B, n))
-    lp, rp = _need("lens", lens, torch.int32, (B,)), _need("row_map", row_map, torch.int32, (B, n))
+    dev = _device("acc", acc)
+    ap = _need("acc", acc, torch.float32, (B, n), dev)
+    lp, rp = _need("lens", lens, torch.int32, (B,), dev), _need("row_map", row_map, torch.int32, (B, n), dev)
     left = acc.new_empty((B, max(keep, 0)))
     kept = torch.empty_like(left, dtype=torch.int32)
     kept_rows, new_lens = torch.empty_like(kept), acc.new_empty(B, dtype=torch.int32)
     _check(lib().dllmc_op_evict(ap, B, n, lp, rp, cache_rows, keep, first, last, kept.data_ptr(), kept_rows.data_ptr(),
-                                new_lens.data_ptr(), left.data_ptr(), _stream_handle()), "dllmc_op_evict")
+                                new_lens.data_ptr(), left.data_ptr(), _stream(dev)), "dllmc_op_evict")
     return kept, kept_rows, new_lens, left
 
 
@@ -682,11 +698,13 @@ def op_compact(cache_format: str, rows: torch.Tensor, src_rows: int, H: int, d_h
     is no row leaves row i as it was.  rows: int32 of any shape, taken flat.  Formats: "f32", "bf16", "kv4"."""
     M = rows.numel()
     dst_rows = M if dst_rows is None else dst_rows
-    rp = _need("rows", rows, torch.int32, rows.shape)
-    ks, kd = _need_cache("k_src", cache_format, k_src, src_rows, H, d_h), _need_cache("k_dst", cache_format, k_dst, dst_rows, H, d_h)
-    vs = None if v_src is None else _need_cache("v_src", cache_format, v_src, src_rows, H, d_h)
-    vd = None if v_dst is None else _need_cache("v_dst", cache_format, v_dst, dst_rows, H, d_h)
-    _check(lib().dllmc_op_compact(_format(cache_format), rp, M, src_rows, dst_rows, H, d_h, ks, kd, vs, vd, _stream_handle()),
+    dev = _device("rows", rows)
+    rp = _need("rows", rows, torch.int32, rows.shape, dev)
+    ks = _need_cache("k_src", cache_format, k_src, src_rows, H, d_h, dev)
+    kd = _need_cache("k_dst", cache_format, k_dst, dst_rows, H, d_h, dev)
+    vs = None if v_src is None else _need_cache("v_src", cache_format, v_src, src_rows, H, d_h, dev)
+    vd = None if v_dst is None else _need_cache("v_dst", cache_format, v_dst, dst_rows, H, d_h, dev)
+    _check(lib().dllmc_op_compact(_format(cache_format), rp, M, src_rows, dst_rows, H, d_h, ks, kd, vs, vd, _stream(dev)),
            "dllmc_op_compact")
 
 
@@ -733,9 +751,10 @@ def op_quant8(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = Non
     code, tdt = _DTYPES[dtype]
     K = x.shape[1]
     M = x.shape[0] if row_idx is None else row_idx.numel()
-    xp, rp = _need("x", x, tdt, x.shape), _need("row_idx", row_idx, torch.int32, (M,))
+    dev = _device("x", x)
+    xp, rp = _need("x", x, tdt, x.shape, dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
     q, scale = x.new_empty((M, i8_row_bytes(K)), dtype=torch.int8), x.new_empty(M, dtype=torch.float32)
-    _check(lib().dllmc_op_quant8(code, xp, rp, M, K, q.data_ptr(), scale.data_ptr(), _stream_handle()), "dllmc_op_quant8")
+    _check(lib().dllmc_op_quant8(code, xp, rp, M, K, q.data_ptr(), scale.data_ptr(), _stream(dev)), "dllmc_op_quant8")
     return q, scale
 
 
@@ -744,12 +763,13 @@ def op_linear_i8(dtype: str, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Te
     """[M, N] of dtype: rows a times rows w (both as op_quant8 gives them, K integers each), scales multiplied in."""
     code, tdt = _DTYPES[dtype]
     M, N, kp = a.shape[0], w.shape[0], i8_row_bytes(K)
-    ap, wp = _need("a", a, torch.int8, (M, kp)), _need("w", w, torch.int8, (N, kp))
-    sa, sw = _need("a_scale", a_scale, torch.float32, (M,)), _need("w_scale", w_scale, torch.float32, (N,))
+    dev = _device("a", a)
+    ap, wp = _need("a", a, torch.int8, (M, kp), dev), _need("w", w, torch.int8, (N, kp), dev)
+    sa, sw = _need("a_scale", a_scale, torch.float32, (M,), dev), _need("w_scale", w_scale, torch.float32, (N,), dev)
     out = a.new_empty((M, N), dtype=tdt)
     nbytes = _scratch_bytes("linear_i8", M, N, K)
     scratch = _scratch(nbytes, out)
-    _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream_handle()),
+    _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream(dev)),
            "dllmc_op_linear_i8")
     return out
 
