@@ -103,6 +103,9 @@ struct AttendItem { int b, h, tile, range, local; };  // range < 0: all keys
 // k_attend_few<T, D, QB, NW>: 16 QB rows of one KV head against a range of keys.  The NW wavefronts deal the range's 32-key blocks
 // among themselves; each carries all the rows, keeps the next block in registers while it works on this one, and meets the
 // others in LDS at the end.  V is expanded into a tile of the wavefront's own in LDS and comes back transposed.
+// Bound by the sum of its instructions with two wavefronts per SIMD (51 rows x 4608 keys: vector ALU 56 % of the time, matrix pipes 21 %,
+// LDS 45 %), then the first loads and the hand-over.  Keys loaded along the rows and turned in LDS, queries loaded once for all wavefronts,
+// scalar addresses for whole blocks: each within 3 % either way; sixteen wavefronts (128 registers): 21 to 32 us.
 template <typename T, int D, int QB, int NW, bool PAGED>
 __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const AttendShape& s, KeyLoader<D, PAGED> ld,
                                                 const AttendItem& it, T* __restrict__ out, float* __restrict__ lse,
@@ -643,9 +646,9 @@ __global__ __launch_bounds__(256) void k_attend_merge(const float* __restrict__ 
 // wavefront walks x block (one after the other) and x share (per workgroup of a CU) + MB of the caches x mb; and where items are cut
 // the joining launch: cut + MB of partial results x part + ranges x range.  Fitted (5 to 13 % rms) to 5600 launches of 419 shapes, 1 to
 // 4608 rows, 96 to 16384 keys, 1 to 16 sequences; the choices are 1.3 % from the quickest on average.  Us (heads of 128): one row x 4608
-// keys x 32 heads 12.6, 51 rows 19.8, 16 sequences x 1 row x 4099 keys x 28 / 4 heads in pages 17.4, 4608 rows x 4608 keys x 32 heads 431
-// (0.81 PFLOP/s, 1.21 with the remainders' products): two and a quarter rounds of 256 workgroups, of which the quarter
-// is cut in four.
+// keys x 32 heads 12.5, 51 rows 19 to 21 (by what the caches hold), 16 sequences x 1 row x 4099 keys x 28 / 4 heads in pages 16.7, 4608 rows
+// x 4608 keys x 32 heads 448 (0.78 PFLOP/s, 1.17 with the remainders' products): two and a quarter rounds of 256 workgroups, of which the
+// quarter is cut in four.
 struct AttendCost { int d, f32, rows, waves, groups; double start, round, block, share, mb, cut, part, range; };
 constexpr AttendCost kAttendCosts[] = {
     {64, 1, 16, 4, 5, 2.78, 0.56, 0.258, 0.406, 0, 2.68, 0.521, 0.268},

@@ -14,7 +14,7 @@ namespace {
 
 // ---- rows in and out -------------------------------------------------------------------------------
 // Four lanes take a block, eight elements each: one 16-byte load of bf16 (two of float32), a maximum over the quad
-// by lane moves, four bytes of codes.  Bound by the bytes: 64.5 bits an element in and out of a bf16 row.
+// by lane moves, four bytes of codes.  Bound by the bytes: 20.25 bits an element in and out of a bf16 row.
 // A thread takes kTrips pieces of eight elements, a workgroup's 256 apart, all loaded before the first is used.
 constexpr int kTrips = 4;
 
