@@ -462,7 +462,7 @@ int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32
                      int32_t d_h, const void* k_src, void* k_dst, const void* v_src, void* v_dst, void* hip_stream);
 
 /* Rows in 8-bit integers: dllmc_i8_row_bytes(K) bytes each, K rounded up to 128 (K <= 131072; 0: invalid), zeros behind the K-th.
- * q[i][k] = the integer nearest to the float32 product x[r][k] * (127 / max|x[r]|), ties to even, scale[i] = max|x[r]| / 127, r =
+ * q[i][k] = the integer nearest to the float32 product x[r][k] * f, ties to even, f = 127 * (1 / max|x[r]|), scale[i] = max|x[r]| / 127, r =
  * row_idx[i] (i if NULL).  A row whose maximum is below 2^-118 becomes zeros with scale 0, one with an infinity or NaN zeros with
  * scale NaN.  For weights (rows = output channels) as for activations (rows = tokens). */
 size_t dllmc_i8_row_bytes(int32_t K);

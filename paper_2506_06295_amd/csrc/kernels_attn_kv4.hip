@@ -105,7 +105,7 @@ struct AttendItem { int b, h, tile, range, local; };  // range < 0: all keys
 // others in LDS at the end.  V is expanded into a tile of the wavefront's own in LDS and comes back transposed.
 // Bound by the sum of its instructions with two wavefronts per SIMD (51 rows x 4608 keys: vector ALU 56 % of the time, matrix pipes 21 %,
 // LDS 45 %), then the first loads and the hand-over.  Keys loaded along the rows and turned in LDS, queries loaded once for all wavefronts,
-// scalar addresses for whole blocks: each within 3 % either way; sixteen wavefronts (128 registers): 21 to 32 us.
+// scalar addresses for whole blocks: each within 4 % either way; sixteen wavefronts (128 registers): 21 to 32 us.
 template <typename T, int D, int QB, int NW, bool PAGED>
 __device__ __forceinline__ void attend_few_body(const T* __restrict__ q, const AttendShape& s, KeyLoader<D, PAGED> ld,
                                                 const AttendItem& it, T* __restrict__ out, float* __restrict__ lse,

@@ -18,7 +18,7 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // ---- quantising rows --------------------------------------------------------------------------------------
-// Rows below this largest magnitude count as zeros: 127 / it stays finite.
+// Rows below this largest magnitude count as zeros: 127 times its reciprocal stays finite.
 constexpr float kTiny = 1.17549435e-38f * 256.f;
 
 struct RowScale {
@@ -28,7 +28,7 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   const float m = __uint_as_float(top);
   const bool finite = top < 0x7f800000u, some = finite && m >= kTiny;
-  return {some ? 127.f / m : 0.f, !finite ? __uint_as_float(0x7fc00000u) : some ? m / 127.f : 0.f, finite};
+  return {some ? 127.f * (1.f / m) : 0.f, !finite ? __uint_as_float(0x7fc00000u) : some ? m / 127.f : 0.f, finite};
 }
 template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
 #pragma unroll
@@ -41,7 +41,8 @@ template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint
   return v;
 }
 
-// q = rint(x * (127 / max|x|)), scale = max|x| / 127; one workgroup per row, the row in registers (PC pieces of eight elements a
+// q = rint(x * (127 * (1 / max|x|))) in float32 (what 127 / tensor is where a tensor's reciprocal is multiplied: the same codes as a
+// plain program's), scale = max|x| / 127; one workgroup per row, the row in registers (PC pieces of eight elements a
 // thread).  Bound by the bytes with many rows, by two trips to memory with few.
 template <typename T, int PC>
 __global__ __launch_bounds__(256) void k_quant8(const T* __restrict__ x, const int* __restrict__ rows, int K, int Kp,

@@ -158,7 +158,7 @@ def quant8(x):
         if top < 2.0 ** -118:
             continue
         scale[i] = np.float32(top / np.float32(127))
-        q[i] = np.rint(row * np.float32(np.float32(127) / top)).astype(np.int64)
+        q[i] = np.rint(row * np.float32(np.float32(127) * np.float32(np.float32(1) / top))).astype(np.int64)
     return q, scale
 
 
