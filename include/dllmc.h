@@ -424,8 +424,8 @@ int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int3
 /* Cached keys of the operations below: sequence b has the positions j < lens[b] (n if lens is NULL; values outside [0, n] count
  * as the nearest of the two), position j in cache row row_map[b * n + j] (b * n + j if row_map is NULL).  A position whose entry is
  * no row of the cache is not there.  What lies in rows and positions that are not there has no influence whatever it
- * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements; at most 2^24 positions and 2^23 rows of B * Mq *
- * H_q.
+ * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements; B <= 65536, B * n <= 2^24 positions, fewer than 2^23
+ * rows B * Mq * H_q.
  *
  * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
  * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without
@@ -438,8 +438,8 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
                            int32_t H_kv, int32_t d_h, void* out, float* lse, void* scratch, size_t scratch_bytes,
                            void* hip_stream);
 /* Attention weight of every cached position: acc_out[b][j] = acc_in[b][j] (0 if NULL; may be acc_out) + the sum over the Mq
- * queries and H_q heads of their softmax probabilities, float32 [B, n]; positions that are not there get nothing.  k_cache:
- * [cache_rows, H_kv * d_h] in the dtype of q (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what
+ * queries and H_q heads of their softmax probabilities, float32 [B, n], B * n * H_kv <= 2^30; positions that are not there get
+ * nothing.  k_cache: [cache_rows, H_kv * d_h] in the dtype of q (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what
  * dllmc_op_attention_kv4 gave for these operands, or NULL (then it is worked out first: beyond 1024 keys at most they are read
  * twice).  Bit-reproducible. */
 size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n,
@@ -462,11 +462,12 @@ int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32
                      int32_t d_h, const void* k_src, void* k_dst, const void* v_src, void* v_dst, void* hip_stream);
 
 /* Rows in 8-bit integers: dllmc_i8_row_bytes(K) bytes each, K rounded up to 128 (K <= 131072; 0: invalid), zeros behind the K-th.
- * q[i][k] = the integer nearest to the float32 product x[r][k] * f, ties to even, f = 127 * (1 / max|x[r]|), scale[i] = max|x[r]| / 127, r =
- * row_idx[i] (i if NULL).  A row whose maximum is below 2^-118 becomes zeros with scale 0, one with an infinity or NaN zeros with
- * scale NaN.  For weights (rows = output channels) as for activations (rows = tokens). */
+ * q[i][k] = the integer nearest to the float32 product x[r][k] * f, ties to even, f = 127 * (1 / max|x[r]|), scale[i] =
+ * max|x[r]| / 127, r = row_idx[i] (i if NULL), x [x_rows, K], aligned to its elements.  A row whose maximum is below 2^-118, and an
+ * r outside [0, x_rows), becomes zeros with scale 0; a row with an infinity or NaN zeros with scale NaN.  For weights (rows =
+ * output channels) as for activations (rows = tokens). */
 size_t dllmc_i8_row_bytes(int32_t K);
-int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
+int dllmc_op_quant8(int32_t dtype, const void* x, int32_t x_rows, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
                     void* hip_stream);
 /* out[i][j] = a_scale[i] * w_scale[j] * (sum over k of a[i][k] * w[j][k], in integers), [M, N] of dtype; a and w as dllmc_op_quant8
  * leaves them, M <= 2^22, N <= 2^24.  scratch: at least dllmc_op_linear_i8_scratch_bytes() bytes, which may be 0.  Bit-reproducible. */

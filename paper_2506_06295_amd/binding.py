@@ -209,7 +209,7 @@ def lib() -> C.CDLL:
                 ("dllmc_op_evict", C.c_int, [ptr, i32, i32, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr, ptr, ptr]),
                 ("dllmc_op_compact", C.c_int, [i32, ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, ptr]),
                 ("dllmc_i8_row_bytes", size, [i32]),
-                ("dllmc_op_quant8", C.c_int, [i32, ptr, ptr, i32, i32, ptr, ptr, ptr]),
+                ("dllmc_op_quant8", C.c_int, [i32, ptr, i32, ptr, i32, i32, ptr, ptr, ptr]),
                 ("dllmc_op_linear_i8_scratch_bytes", size, [i32] * 3),
                 ("dllmc_plan_attention_kv4", i32, [i32] * 7 + [C.POINTER(i32)] * 3),
                 ("dllmc_plan_attention_weights", i32, [i32] * 8 + [C.POINTER(i32)] * 3),
@@ -747,14 +747,15 @@ def plan_linear_i8(M: int, N: int, K: int):
 
 
 def op_quant8(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = None):
-    """(int8 [M, i8_row_bytes(K)], float32 [M]): rows of x [*, K] (those that row_idx int32 [M] names) and their scales."""
+    """(int8 [M, i8_row_bytes(K)], float32 [M]): rows of x [*, K] (those that row_idx int32 [M] names, zeros where it names none) and
+    their scales."""
     code, tdt = _DTYPES[dtype]
     K = x.shape[1]
     M = x.shape[0] if row_idx is None else row_idx.numel()
     dev = _device("x", x)
     xp, rp = _need("x", x, tdt, x.shape, dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
     q, scale = x.new_empty((M, i8_row_bytes(K)), dtype=torch.int8), x.new_empty(M, dtype=torch.float32)
-    _check(lib().dllmc_op_quant8(code, xp, rp, M, K, q.data_ptr(), scale.data_ptr(), _stream(dev)), "dllmc_op_quant8")
+    _check(lib().dllmc_op_quant8(code, xp, x.shape[0], rp, M, K, q.data_ptr(), scale.data_ptr(), _stream(dev)), "dllmc_op_quant8")
     return q, scale
 
 

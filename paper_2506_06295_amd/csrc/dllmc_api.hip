@@ -1161,7 +1161,7 @@ inline size_t elem_bytes(int32_t dtype) { return dtype == DLLMC_BF16 ? 2 : 4; }
 
 constexpr int kMaxRows = 1 << 24;  // rows of a cache, positions of a batch (as for a context)
 constexpr int kMaxWidth = 1 << 16;  // H * d_h
-constexpr int kMaxBatch = 1 << 16;   // (a launch has at most 2^32 work-items)
+constexpr int kMaxBatch = 1 << 16;   // (a launch has fewer than 2^32 work-items: 2^23 workgroups of 512)
 constexpr int kMaxI8M = 1 << 22;     // (row tiles in y: at most 2^16)
 constexpr int kMaxI8K = 1 << 17;   // 127 * 127 * 2^17 < 2^31: a whole contraction fits an int32 sum
 
@@ -1174,10 +1174,13 @@ bool attend_shape_ok(int32_t B, int32_t Mq, int32_t cache_rows, const int32_t* r
                      int32_t H_kv, int32_t d_h) {
   if (B < 1 || Mq < 1 || n < 1 || H_kv < 1 || H_q < H_kv || H_q % H_kv || (d_h != 64 && d_h != 128 && d_h != 256)) return false;
   if (cache_rows < 1 || cache_rows > kMaxRows || n > kMaxRows / B || H_q > kMaxWidth / d_h || Mq > kMaxRows / B) return false;
-  if (B > kMaxBatch || static_cast<long long>(B) * Mq * H_q > (1ll << 23)) return false;
+  if (B > kMaxBatch || static_cast<long long>(B) * Mq * H_q >= (1ll << 23)) return false;
   if (row_map == nullptr && static_cast<long long>(B) * n > cache_rows) return false;
   return aligned4(row_map) && aligned4(lens);
 }
+
+// partial column sums: 4 GB a row share, and 2^24 workgroups
+bool weigh_shape_ok(int32_t B, int32_t n, int32_t H_kv) { return static_cast<long long>(B) * n * H_kv <= (1ll << 30); }
 
 size_t cache_bytes(int32_t format, int32_t rows, int32_t H, int32_t d_h) {
   return format == DLLMC_KV4 ? kv4_bytes(rows, H, d_h) : static_cast<size_t>(rows) * H * d_h * elem_bytes(format);
@@ -1262,7 +1265,7 @@ size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_for
                                                 int32_t H_kv, int32_t d_h) {
   static const int32_t some = 0;
   if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) ||
-      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h))
+      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h) || !weigh_shape_ok(B, n, H_kv))
     return 0;
   return attention_weights_scratch_bytes(plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h), B, Mq, n, H_q, H_kv);
 }
@@ -1272,7 +1275,7 @@ int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* 
                                int32_t d_h, const float* lse, const float* acc_in, float* acc_out, void* scratch,
                                size_t scratch_bytes, void* hip_stream) {
   if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) || !q || !k_cache || !acc_out ||
-      !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !aligned16(q) || !aligned16(k_cache) ||
+      !attend_shape_ok(B, Mq, cache_rows, row_map, lens, n, H_q, H_kv, d_h) || !weigh_shape_ok(B, n, H_kv) || !aligned16(q) || !aligned16(k_cache) ||
       !aligned4(lse) || !aligned4(acc_in) || !aligned4(acc_out) || !aligned16(scratch))
     return DLLMC_EINVAL;
   const WeighPlan plan = plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
@@ -1344,19 +1347,17 @@ int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32
 
 size_t dllmc_i8_row_bytes(int32_t K) { return K >= 1 && K <= kMaxI8K ? i8_row_bytes(K) : 0; }
 
-int dllmc_op_quant8(int32_t dtype, const void* x, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
+int dllmc_op_quant8(int32_t dtype, const void* x, int32_t x_rows, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
                     void* hip_stream) {
-  if (!dtype_ok(dtype) || !x || !q || !scale || M < 1 || M >= kMaxRows || K < 1 || K > kMaxI8K || !aligned16(q) || !aligned4(scale) ||
-      !aligned4(row_idx) || reinterpret_cast<uintptr_t>(x) % elem_bytes(dtype))
+  if (!dtype_ok(dtype) || !x || !q || !scale || M < 1 || M >= kMaxRows || x_rows < 1 || (row_idx == nullptr && M > x_rows) || K < 1 ||
+      K > kMaxI8K || !aligned16(q) || !aligned4(scale) || !aligned4(row_idx) || reinterpret_cast<uintptr_t>(x) % elem_bytes(dtype))
     return DLLMC_EINVAL;
-  const size_t qb = M * i8_row_bytes(K), sb = static_cast<size_t>(M) * 4;
-  // (a gathered x has more rows than the call says: it has to lie clear of both results in the rows it names, which is the caller's to see to)
-  const size_t xb = (row_idx ? 1 : static_cast<size_t>(M)) * K * elem_bytes(dtype);
+  const size_t qb = M * i8_row_bytes(K), sb = static_cast<size_t>(M) * 4, xb = static_cast<size_t>(x_rows) * K * elem_bytes(dtype);
   if (!apart(q, qb, x, xb) || !apart(scale, sb, x, xb) || !apart(q, qb, scale, sb) ||
       (row_idx && (!apart(q, qb, row_idx, sb) || !apart(scale, sb, row_idx, sb))))
     return DLLMC_EINVAL;
   (void)hipGetLastError();
-  launch_quant8(dtype, x, row_idx, M, K, q, scale, static_cast<hipStream_t>(hip_stream));
+  launch_quant8(dtype, x, x_rows, row_idx, M, K, q, scale, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
   return DLLMC_OK;
 }
@@ -1376,7 +1377,7 @@ int32_t dllmc_plan_attention_weights(int32_t dtype, int32_t cache_format, int32_
                                      int32_t d_h, int32_t* ranges, int32_t* row_blocks, int32_t* shares) {
   static const int32_t some = 0;
   if (!dtype_ok(dtype) || (cache_format != dtype && cache_format != DLLMC_KV4) ||
-      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h))
+      !attend_shape_ok(B, Mq, 1, &some, nullptr, n, H_q, H_kv, d_h) || !weigh_shape_ok(B, n, H_kv))
     return DLLMC_EINVAL;
   const WeighPlan p = plan_weigh(dtype, cache_format, B, Mq, n, H_q, H_kv, d_h);
   if (ranges) *ranges = p.brief ? 0 : p.s.KS;
@@ -1403,7 +1404,7 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
                        int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes, void* hip_stream) {
   if (!dtype_ok(dtype) || !a || !a_scale || !w || !w_scale || !out || M < 1 || M > kMaxI8M || N < 1 || N > kMaxRows || K < 1 ||
       K > kMaxI8K || !aligned16(a) || !aligned16(w) || !aligned4(a_scale) || !aligned4(w_scale) ||
-      reinterpret_cast<uintptr_t>(out) % elem_bytes(dtype) || !aligned16(scratch))
+      !aligned16(out) || !aligned16(scratch))
     return DLLMC_EINVAL;
   const size_t kp = i8_row_bytes(K);
   const I8Plan plan = plan_i8(M, N, static_cast<int>(kp));

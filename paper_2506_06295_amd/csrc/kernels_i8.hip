@@ -45,16 +45,17 @@ template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint
 // plain program's), scale = max|x| / 127; one workgroup per row, the row in registers (PC pieces of eight elements a
 // thread).  Bound by the bytes with many rows, by two trips to memory with few.
 template <typename T, int PC>
-__global__ __launch_bounds__(256) void k_quant8(const T* __restrict__ x, const int* __restrict__ rows, int K, int Kp,
+__global__ __launch_bounds__(256) void k_quant8(const T* __restrict__ x, int x_rows, const int* __restrict__ rows, int K, int Kp,
                                                 int8_t* __restrict__ q, float* __restrict__ scale) {
   __shared__ uint32_t red[4];
   const int i = blockIdx.x;
-  const T* r = x + static_cast<size_t>(rows ? rows[i] : i) * K;
+  const int row = rows ? rows[i] : i, len = static_cast<unsigned>(row) < static_cast<unsigned>(x_rows) ? K : 0;  // (no row: zeros)
+  const T* r = x + static_cast<size_t>(len ? row : 0) * K;
   float v[PC][8];
 #pragma unroll
   for (int p = 0; p < PC; ++p) {
     const int t = (p * 256 + threadIdx.x) * 8;
-    if (t < K) {
+    if (t < len) {
       Eight<T>::load(r + t, v[p]);
     } else {
 #pragma unroll
@@ -83,13 +84,14 @@ __global__ __launch_bounds__(256) void k_quant8(const T* __restrict__ x, const i
 
 // any K and alignment, the row read twice
 template <typename T>
-__global__ __launch_bounds__(256) void k_quant8_any(const T* __restrict__ x, const int* __restrict__ rows, int K, int Kp,
+__global__ __launch_bounds__(256) void k_quant8_any(const T* __restrict__ x, int x_rows, const int* __restrict__ rows, int K, int Kp,
                                                     int8_t* __restrict__ q, float* __restrict__ scale) {
   __shared__ uint32_t red[4];
   const int i = blockIdx.x;
-  const T* r = x + static_cast<size_t>(rows ? rows[i] : i) * K;
+  const int row = rows ? rows[i] : i, len = static_cast<unsigned>(row) < static_cast<unsigned>(x_rows) ? K : 0;  // (no row: zeros)
+  const T* r = x + static_cast<size_t>(len ? row : 0) * K;
   uint32_t top = 0;
-  for (int t = threadIdx.x; t < K; t += 256) top = max(top, __float_as_uint(ldf(r + t)) & 0x7fffffffu);
+  for (int t = threadIdx.x; t < len; t += 256) top = max(top, __float_as_uint(ldf(r + t)) & 0x7fffffffu);
   const RowScale s = row_scale(block_max<4>(top, red));
   if (threadIdx.x == 0) scale[i] = s.scale;
   uint32_t* o = reinterpret_cast<uint32_t*>(q + static_cast<size_t>(i) * Kp);
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(256) void k_quant8_any(const T* __restrict__ x, con
     uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (s.finite && 4 * t + e < K) w |= (static_cast<uint32_t>(static_cast<int>(rintf(ldf(r + 4 * t + e) * s.f))) & 255u) << (e * 8);
+      if (s.finite && 4 * t + e < len) w |= (static_cast<uint32_t>(static_cast<int>(rintf(ldf(r + 4 * t + e) * s.f))) & 255u) << (e * 8);
     o[t] = w;
   }
 }
@@ -549,11 +551,11 @@ void launch_i8(const I8Plan& p, const int8_t* a, const float* sa, int M, const i
 }
 
 template <typename T>
-void quant8(const T* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
+void quant8(const T* x, int x_rows, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
   const int Kp = static_cast<int>(i8_row_bytes(K));
   const bool pieces = K % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
-#define DLLMC_Q(PC) hipLaunchKernelGGL((k_quant8<T, PC>), dim3(M), dim3(256), 0, st, x, rows, K, Kp, q, scale)
-  if (!pieces || K > 2048 * 10) hipLaunchKernelGGL(k_quant8_any<T>, dim3(M), dim3(256), 0, st, x, rows, K, Kp, q, scale);
+#define DLLMC_Q(PC) hipLaunchKernelGGL((k_quant8<T, PC>), dim3(M), dim3(256), 0, st, x, x_rows, rows, K, Kp, q, scale)
+  if (!pieces || K > 2048 * 10) hipLaunchKernelGGL(k_quant8_any<T>, dim3(M), dim3(256), 0, st, x, x_rows, rows, K, Kp, q, scale);
   else if (Kp <= 2048) DLLMC_Q(1);
   else if (Kp <= 4096) DLLMC_Q(2);
   else if (Kp <= 12288) DLLMC_Q(6);
@@ -571,6 +573,7 @@ I8Plan plan_i8(int M, int N, int Kp) {
   for (const I8Cost& c : kI8Costs) {
     const long long mt = (M + c.bm - 1) / c.bm, nt = (N + c.bn - 1) / c.bn;
     if (mt > 65535) continue;  // (the grid's second dimension)
+    if ((M + c.bm - 1) / c.bm > 65535) continue;  // (a launch's tiles in y)
     for (const int S : {1, 2, 3, 4, 6, 8}) {
       if (S > 1 && (c.wide || S > lines)) break;
       const int per = (lines + S - 1) / S, used = (lines + per - 1) / per;
@@ -585,9 +588,9 @@ I8Plan plan_i8(int M, int N, int Kp) {
   return best;
 }
 
-void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
-  if (dtype == 1) quant8(static_cast<const bf16_t*>(x), rows, M, K, q, scale, st);
-  else quant8(static_cast<const float*>(x), rows, M, K, q, scale, st);
+void launch_quant8(int dtype, const void* x, int x_rows, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
+  if (dtype == 1) quant8(static_cast<const bf16_t*>(x), x_rows, rows, M, K, q, scale, st);
+  else quant8(static_cast<const float*>(x), x_rows, rows, M, K, q, scale, st);
 }
 
 size_t linear_i8_scratch_bytes(const I8Plan& p, int M, int N) {

@@ -175,7 +175,7 @@ void launch_compact(int format, const int* rows, int M, int src_rows, int dst_ro
 
 // 8-bit rows of K rounded up to 128 bytes (kernels_i8.hip)
 inline size_t i8_row_bytes(int K) { return (static_cast<size_t>(K) + 127) / 128 * 128; }
-void launch_quant8(int dtype, const void* x, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st);
+void launch_quant8(int dtype, const void* x, int x_rows, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st);
 struct I8Plan { int wide, bm, bn, S, per; };  // wide: tile kernel; else ring of bm x bn and S slices of `per` bytes
 I8Plan plan_i8(int M, int N, int Kp);
 size_t linear_i8_scratch_bytes(const I8Plan& p, int M, int N);

@@ -345,6 +345,9 @@ def test_quant8(dtype, M, K):
         assert np.array_equal(scale.cpu().numpy(), s, equal_nan=True)
         got = got.cpu().numpy()
         assert np.array_equal(got[:, :K], q) and (got[:, K:] == 0).all()
+    got, scale = L.op_quant8(dtype, R.dev(x, dtype), row_idx=R.ints([-1, 0, M + 4, -2 ** 31, 2 ** 31 - 1]))  # what is no row
+    assert (scale[[0, 2, 3, 4]] == 0).all() and (got[[0, 2, 3, 4]] == 0).all()
+    assert np.array_equal(got[1, :K].cpu().numpy(), R.quant8(x[:1])[0][0])
 
 
 def check_linear(dtype, M, N, K, seed=0, extreme=False):

@@ -367,6 +367,26 @@ def test_plain_rows_past_4_gib():
     assert torch.equal(L.op_linear_i8("f32", big, scale, w, sw, H * d_h)[rows.long()], L.op_linear_i8("f32", few, few_scale, w, sw, H * d_h))
 
 
+def test_largest_batch():
+    """65535 sequences of 128 heads, one workgroup each: as many as a launch takes.  With one key in two there all is exact."""
+    B, H, d_h, R_ = 65535, 128, 64, 96
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    k, v = (torch.zeros(L.kv4_bytes(R_, H, d_h), dtype=torch.uint8, device="cuda") for _ in range(2))
+    for c in (k, v):
+        L.op_kv4_store("bf16", torch.randn(R_, H * d_h, generator=g, device="cuda").to(torch.bfloat16), c, R_, H, d_h)
+    q = torch.randn(B, 1, H * d_h, generator=g, device="cuda", dtype=torch.bfloat16)
+    m = torch.randint(0, R_, (B, 2), generator=g, device="cuda", dtype=torch.int32)
+    m[torch.arange(B, device="cuda"), m[:, 0] % 2] = -1
+    at = m.amax(1).long()
+    out = L.op_attention_kv4("bf16", q, k, v, R_, 2, H, H, d_h, row_map=m)
+    values = L.op_kv4_load("bf16", v, R_, H, d_h)
+    for i in range(0, B, 8192):
+        assert torch.equal(out[i:i + 8192, 0], values[at[i:i + 8192]])
+    del out
+    assert torch.equal(L.op_attention_weights("bf16", "kv4", q, k, R_, 2, H, H, d_h, row_map=m), H * (m >= 0).float())
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_binding_refuses():
     f = torch.zeros

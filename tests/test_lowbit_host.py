@@ -1,6 +1,7 @@
 """Refusals of the operators in fewer bits, and the sizes they state: no GPU needed, nothing is launched."""
 import ctypes
 import os
+import random
 
 import pytest
 
@@ -43,7 +44,7 @@ EVICT = dict(acc=p(0), B=2, n=50, lens=p(1), row_map=p(2), cache_rows=100, keep=
              new_lens=p(5), acc_out=p(6), stream=None)
 COMPACT = dict(fmt=BF16, rows=p(0), M=5, src_rows=9, dst_rows=7, H=2, d_h=64, k_src=p(1), k_dst=p(2), v_src=p(3), v_dst=p(4),
                stream=None)
-QUANT = dict(dtype=BF16, x=p(0), rows=p(1), M=4, K=100, q=p(2), scale=p(3), stream=None)
+QUANT = dict(dtype=BF16, x=p(0), x_rows=9, rows=p(1), M=4, K=100, q=p(2), scale=p(3), stream=None)
 LINEAR = dict(dtype=BF16, a=p(0), sa=p(1), M=4, w=p(2), sw=p(3), N=8, K=100, out=p(4), scratch=p(5), nbytes=1 << 36, stream=None)
 
 
@@ -78,11 +79,11 @@ BAD = {
     "dllmc_op_compact": [dict(fmt=3), dict(rows=None), dict(k_src=None), dict(k_dst=None), dict(v_src=None), dict(v_dst=None), dict(M=0),
                          dict(M=8), dict(src_rows=0), dict(H=0), dict(d_h=0), dict(fmt=KV4, d_h=40), dict(k_dst=p(1)), dict(v_dst=p(2)),
                          dict(v_dst=p(1)), dict(k_dst=p(0)), dict(k_src=near(p(1), 1)), dict(fmt=KV4, k_src=near(p(1), 8))],
-    "dllmc_op_quant8": [dict(dtype=2), dict(x=None), dict(q=None), dict(scale=None), dict(M=0), dict(K=0), dict(K=131073),
+    "dllmc_op_quant8": [dict(dtype=2), dict(x=None), dict(x_rows=0), dict(rows=None, M=10), dict(q=near(p(0), 16 * 100)), dict(q=None), dict(scale=None), dict(M=0), dict(K=0), dict(K=131073),
                         dict(q=near(p(2), 8)), dict(x=near(p(0), 1)), dict(q=p(0)), dict(scale=p(2)), dict(scale=p(0)), dict(q=p(1))],
     "dllmc_op_linear_i8": [dict(dtype=2), dict(a=None), dict(sa=None), dict(w=None), dict(sw=None), dict(out=None), dict(M=0), dict(N=0),
                            dict(K=0), dict(K=131073), dict(a=near(p(0), 8)), dict(w=near(p(2), 4)), dict(out=near(p(4), 1)),
-                           dict(out=p(0)), dict(out=p(2)), dict(out=p(1)), dict(out=p(3))],
+                           dict(out=near(p(4), 8)), dict(out=p(0)), dict(out=p(2)), dict(out=p(1)), dict(out=p(3))],
 }
 
 
@@ -90,6 +91,24 @@ BAD = {
 def test_refused(name, change):
     args = dict(CALLS[name], **change)
     assert getattr(L, name)(*args.values()) == EINVAL
+
+
+def test_largest_shapes():
+    """A launch has fewer than 2^32 work-items: the next larger batch is refused."""
+    for B, ok in ((65535, True), (65536, False)):
+        for n in (1, 128, 200):
+            rows = (BF16, B, 1, n, 128, 128, 64)
+            assert (L.dllmc_plan_attention_kv4(*rows, None, None, None) > 0) == ok
+            fits = ok and B * n * 128 <= 1 << 30
+            assert (L.dllmc_plan_attention_weights(BF16, KV4, *rows[1:], None, None, None) > 0) == fits
+            assert (L.dllmc_op_attention_weights_scratch_bytes(BF16, KV4, *rows[1:]) > 0) == fits
+    assert L.dllmc_plan_attention_weights(BF16, KV4, 1, 1, 1 << 24, 64, 64, 64, None, None, None) > 0
+    assert L.dllmc_plan_attention_weights(BF16, KV4, 1, 1, 1 << 24, 65, 65, 64, None, None, None) == EINVAL
+    r = random.Random(1)
+    for _ in range(4000):
+        M, N, K = min(1 << 22, int(2 ** r.uniform(0, 22.1))), int(2 ** r.uniform(0, 24)), int(2 ** r.uniform(0, 17))
+        (rows, _), _, _ = binding.plan_linear_i8(M, N, K)
+        assert -(-M // rows) <= 65535
 
 
 def test_scratch_too_small():
