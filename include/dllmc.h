@@ -414,7 +414,7 @@ int dllmc_op_attention(int32_t dtype, const void* q, int32_t B, int32_t Mq, cons
  * or NaN and all of it reads as NaN. */
 size_t dllmc_kv4_bytes(int32_t cache_rows, int32_t H, int32_t d_h);
 /* Row rows[i] (i if rows is NULL) of the tensor <- row i of x [M, H * d_h], i < M; entries outside [0, cache_rows) are
- * left out.  A row must not be listed twice (which of the two is kept is undefined then). */
+ * left out.  A row must not be listed twice (what it holds is undefined then). */
 int dllmc_op_kv4_store(int32_t dtype, const void* x, int32_t M, const int32_t* rows, void* cache, int32_t cache_rows,
                        int32_t H, int32_t d_h, void* hip_stream);
 /* out [M, H * d_h] row i = the values of row rows[i] (i if NULL), exact in either dtype; zeros where rows[i] is no row. */
