@@ -623,7 +623,10 @@ WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H
     p.brief = true;
     p.KB = n <= 256 || most == 2 ? 2 : n <= 512 || most == 4 ? 4 : 8;
     const int rt = (s.NR + 15) / 16;
-    long long RS = heads >= 128 ? 1 : 128 / heads;
+    // A workgroup per CU, two where the registers leave room for more: 3 % from the quickest share count on average (40 shapes; half as many
+    // workgroups 8 %, in the worst 2 times as long: a tile of rows is a chain of loads, products, two exchanges and a barrier)
+    const long long target = dtype == 1 && p.KB == 2 ? 512 : 256;
+    long long RS = heads >= target ? 1 : target / heads;
     if (RS > rt) RS = rt;
     s.share = static_cast<int>((rt + RS - 1) / RS);
     s.RS = (rt + s.share - 1) / s.share;
