@@ -6,20 +6,21 @@ namespace dllmc {
 namespace {
 
 // What positions are ordered by: 0 not there, then NaN, then the weights ascending (-0 as 0), then those always kept.
-__device__ __forceinline__ uint32_t keep_key(const float* acc, const Keys& keys, int b, int j, int len, int first, int last) {
-  if (j >= len || keys.row(b, j) < 0) return 0;
-  if (j < first || j >= len - last) return 0xffffffffu;
-  const float w = acc[static_cast<size_t>(b) * keys.n + j] + 0.f;
-  if (w != w) return 1;
+__device__ __forceinline__ uint32_t keep_key(float w, bool there, bool always) {
+  w += 0.f;
   const uint32_t u = __float_as_uint(w);
-  return (u >> 31) ? ~u : u | 0x80000000u;
+  const uint32_t order = w != w ? 1 : (u >> 31) ? ~u : u | 0x80000000u;
+  return !there ? 0 : always ? 0xffffffffu : order;
 }
 
 // One workgroup of W wavefronts per sequence.  Wavefront w takes the positions [w P, (w + 1) P), P = 64 KPT, 64 neighbours at a time, so
 // that the order of positions is the order of (wavefront, trip, lane) and places come from ballots.  The k-th largest key by
 // up to four passes over its bytes, fewer where a pass ends between two bins; each counts the keys that agree with the bytes found so far in
 // a histogram with a column per lane (weights of one sequence share their exponents: in a single column most of a wavefront's
-// adds would meet).  KPT > 0: keys in registers; 0: formed again in every pass (beyond 32768 positions).
+// adds would meet).  KPT > 0: keys, weights and rows in registers; 0: loaded again in every pass (beyond 16384 positions, whose trips would
+// need more registers than sixteen wavefronts have: with their keys alone in them 29606 positions took 40 us, so 44 and 60000 80).  The
+// loads of all trips, or of sixteen, go out before the first is looked at: behind conditions, each waiting for its predecessor, 16 sequences
+// of 4608 took 13.1 us, now 9.8 to 10.9 (4.4 of them the search), one of 16384 18.6 and 14 to 16.
 template <int W, int KPT>
 __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc, Keys keys, int keep, int first, int last,
                                                   int* __restrict__ kept, int* __restrict__ kept_rows, int* __restrict__ new_lens,
@@ -28,31 +29,66 @@ __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc,
   __shared__ __attribute__((aligned(16))) uint32_t hist[256 * 64];
   __shared__ int bins[256], found[3], counts[2][W];
   const int b = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int trips = KPT > 0 ? KPT : (keys.n + kThreads - 1) / kThreads;
+  constexpr int kBatch = 16;  // trips whose loads go out together where not all do
+  const int trips = KPT > 0 ? KPT : (keys.n + kBatch * kThreads - 1) / (kBatch * kThreads) * kBatch;
   const int len = keys.length(b), j0 = wave * trips * 64 + lane;
+  const char* weight = reinterpret_cast<const char*>(acc + static_cast<size_t>(b) * keys.n);
+  const char* map = keys.row_map != nullptr ? reinterpret_cast<const char*>(keys.row_map + static_cast<size_t>(b) * keys.n) : nullptr;
+  auto at = [&](int i) { return static_cast<uint32_t>(min(j0 + i * 64, keys.n - 1)) * 4; };  // (bytes: a scalar base and a 32-bit offset)
+  auto order = [&](int i, float w, int r) {
+    const int j = j0 + i * 64;
+    return keep_key(w, j < len && static_cast<unsigned>(r) < static_cast<unsigned>(keys.cache_rows), j < first || j >= len - last);
+  };
+  // weights and rows of trips i0 .. + N - 1
+  auto load = [&](int i0, auto& w, auto& r) {
+    constexpr int N = sizeof(w) / sizeof(w[0]);
+#pragma unroll
+    for (int u = 0; u < N; ++u) w[u] = *reinterpret_cast<const float*>(weight + at(i0 + u));
+    if (map != nullptr) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) r[u] = *reinterpret_cast<const int*>(map + at(i0 + u));
+    } else {
+#pragma unroll
+      for (int u = 0; u < N; ++u) r[u] = b * keys.n + j0 + (i0 + u) * 64;
+    }
+  };
   uint32_t held[KPT > 0 ? KPT : 1];
-  auto key = [&](int i) -> uint32_t {
-    if constexpr (KPT > 0) return held[i];
-    return keep_key(acc, keys, b, j0 + i * 64, len, first, last);
+  float held_w[KPT > 0 ? KPT : 1];
+  int held_r[KPT > 0 ? KPT : 1];
+  // f(trip, key, weight, row) for all trips
+  auto each_whole = [&](auto&& f) {
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) f(i, held[i], held_w[i], held_r[i]);
+    } else {
+      for (int i0 = 0; i0 < trips; i0 += kBatch) {
+        float w[kBatch];
+        int r[kBatch];
+        load(i0, w, r);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) f(i0 + u, order(i0 + u, w[u], r[u]), w[u], r[u]);
+      }
+    }
   };
   auto each = [&](auto&& f) {
     if constexpr (KPT > 0) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) f(i);
+      for (int i = 0; i < KPT; ++i) f(held[i]);
     } else {
-      for (int i = 0; i < trips; ++i) f(i);
+      each_whole([&](int, uint32_t u, float, int) { f(u); });
     }
   };
   auto clear = [&] {
     for (int t = threadIdx.x; t < 256 * 16; t += kThreads) reinterpret_cast<uint4*>(hist)[t] = make_uint4(0, 0, 0, 0);
   };
   if constexpr (KPT > 0) {
+    load(0, held_w, held_r);
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) held[i] = keep_key(acc, keys, b, j0 + i * 64, len, first, last);
+    for (int i = 0; i < KPT; ++i) held[i] = order(i, held_w[i], held_r[i]);
   }
   clear();
   int mine = 0;
-  each([&](int i) { mine += __popcll(__ballot(key(i) != 0)); });
+  each([&](uint32_t u) { mine += __popcll(__ballot(u != 0)); });
   if (lane == 0) counts[0][wave] = mine;
   __syncthreads();
   int there = 0;
@@ -66,8 +102,7 @@ __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc,
   if (there > keep) {
     int want = k;  // of the keys that agree with the bytes found so far
     for (int shift = 24; shift >= 0; shift -= 8) {
-      each([&](int i) {
-        const uint32_t u = key(i);
+      each([&](uint32_t u) {
         if (u != 0 && (shift == 24 || (u >> (shift + 8)) == (threshold >> (shift + 8)))) atomicAdd(&hist[((u >> shift) & 255) * 64 + lane], 1u);
       });
       __syncthreads();
@@ -119,8 +154,7 @@ __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc,
   }
   // places: of a position that stays, the number of those before it
   int above = 0, equal = 0;
-  each([&](int i) {
-    const uint32_t u = key(i);
+  each([&](uint32_t u) {
     above += __popcll(__ballot(u > threshold));
     equal += __popcll(__ballot(u == threshold && u != 0));
   });
@@ -137,17 +171,15 @@ __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc,
     equal += w < wave ? counts[1][w] : 0;
   }
   const size_t out0 = static_cast<size_t>(b) * keep;
-  each([&](int i) {
-    const uint32_t u = key(i);
+  each_whole([&](int i, uint32_t u, float w, int r) {
     const uint64_t hi = __ballot(u > threshold), eq = __ballot(u == threshold && u != 0);
     const uint64_t below = (1ull << lane) - 1;
     const int hb = above + __popcll(hi & below), eb = equal + __popcll(eq & below);
     if (u > threshold || (u == threshold && u != 0 && eb < quota)) {
       const size_t at = out0 + hb + min(eb, quota);
-      const int j = j0 + i * 64;
-      kept[at] = j;
-      kept_rows[at] = keys.row(b, j);
-      if (acc_out != nullptr) acc_out[at] = acc[static_cast<size_t>(b) * keys.n + j];
+      kept[at] = j0 + i * 64;
+      kept_rows[at] = r;
+      if (acc_out != nullptr) acc_out[at] = w;
     }
     above += __popcll(hi);
     equal += __popcll(eq);
@@ -211,7 +243,6 @@ void launch_evict(const float* acc, int B, const Keys& keys, int keep, int first
   else if (n <= 4096) DLLMC_E(16, 4);
   else if (n <= 8192) DLLMC_E(16, 8);
   else if (n <= 16384) DLLMC_E(16, 16);
-  else if (n <= 32768) DLLMC_E(16, 32);
   else DLLMC_E(16, 0);
 #undef DLLMC_E
 }
