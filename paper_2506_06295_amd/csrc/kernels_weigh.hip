@@ -595,17 +595,26 @@ __global__ __launch_bounds__(1024) void k_weigh_sum(const float* __restrict__ pa
   __shared__ float red[16][64];
   const int per = (n + 63) / 64, b = blockIdx.x / per, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int j = blockIdx.x % per * 64 + lane;
+  const int at = min(j, n - 1), parts = shares * H;
+  auto load = [&](int p) { return part[(static_cast<size_t>(p / H * B + b) * H + p % H) * n + at]; };
   float sum = 0.f;
-  if (j < n)
-    for (int p = wave; p < shares * H; p += 16) sum += part[(static_cast<size_t>(p / H * B + b) * H + p % H) * n + j];
+  int p = wave;
+  for (; p + 112 < parts; p += 128) {  // (eight loads in flight: of 128 parts one after the other a microsecond)
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = load(p + 16 * u);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += v[u];
+  }
+  for (; p < parts; p += 16) sum += load(p);
   red[wave][lane] = sum;
   __syncthreads();
   if (wave != 0 || j >= n) return;
   sum = 0.f;
 #pragma unroll
   for (int w = 0; w < 16; ++w) sum += red[w][lane];
-  const size_t at = static_cast<size_t>(b) * n + j;
-  acc_out[at] = (acc_in != nullptr ? acc_in[at] : 0.f) + sum;
+  const size_t to = static_cast<size_t>(b) * n + j;
+  acc_out[to] = (acc_in != nullptr ? acc_in[to] : 0.f) + sum;
 }
 
 // most 16s of keys a wavefront's registers hold: fragments of at most 128 of them

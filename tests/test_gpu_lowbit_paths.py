@@ -163,6 +163,25 @@ def test_evict_register_classes(n):
             assert np.array_equal(g.cpu().numpy(), w)
 
 
+@pytest.mark.parametrize("n", [700, 17000, 40000])
+def test_evict_pages_and_holes(n):
+    """Lengths, rows from pages, entries that are no row, NaN and infinite weights: keys in registers and loaded again."""
+    r = np.random.default_rng(n)
+    B, rows = 3, 2 * n
+    acc = R.grid(r.exponential(1.0, (B, n)), "f32")
+    acc[1, r.integers(0, n, 50)] = np.nan
+    acc[2, r.integers(0, n, 50)] = np.inf
+    m = r.integers(0, rows, (B, n)).astype(np.int32)
+    m[r.random((B, n)) < 0.3] = -1
+    m[0, :20] = rows
+    lens = np.array([n - 7, n, 0], np.int32)
+    for keep in (5, n // 2, n):
+        got = L.op_evict(R.dev(acc), keep, rows, 2, 3, lens=R.ints(lens), row_map=R.ints(m))
+        want = R.evict(acc, keep, R.present(B, n, rows, lens, m), lens, n, 2, 3)
+        for g, w in zip(got, want):
+            assert np.array_equal(g.cpu().numpy(), w, equal_nan=g.dtype == torch.float32)
+
+
 # ------------------------------------------------------------------ together
 class Layer:
     """Projections in 8 bits fill a 4-bit cache, rows attend, positions accumulate weight, the cache is halved, the rest attends again."""
