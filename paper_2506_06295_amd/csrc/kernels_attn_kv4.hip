@@ -668,7 +668,7 @@ constexpr AttendCost kAttendCosts[] = {
 };
 }  // namespace
 
-AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
+static AttendPlan choose_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
   const int NR = Mq * (H_q / H_kv);
   const double mb = 2.0 * B * n * H_kv * (d_h / 2 + d_h / 32) / 1e6;
   AttendPlan best{};
@@ -708,6 +708,10 @@ AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d
     }
   }
   return best;
+}
+
+AttendPlan plan_attend(int dtype, int B, int Mq, int n, int H_q, int H_kv, int d_h) {
+  return last_plan<AttendPlan>({dtype, B, Mq, n, H_q, H_kv, d_h}, [&] { return choose_attend(dtype, B, Mq, n, H_q, H_kv, d_h); });
 }
 
 size_t attention_kv4_scratch_bytes(const AttendPlan& p, int d_h) {

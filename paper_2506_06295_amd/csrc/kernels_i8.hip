@@ -565,7 +565,7 @@ void quant8(const T* x, int x_rows, const int* rows, int M, int K, int8_t* q, fl
 
 }  // namespace
 
-I8Plan plan_i8(int M, int N, int Kp) {
+static I8Plan choose_i8(int M, int N, int Kp) {
   const int lines = Kp / 128;
   const double mb_w = static_cast<double>(N) * Kp / 1e6, mn = static_cast<double>(M) * N / 1e6;
   I8Plan best{};
@@ -573,7 +573,6 @@ I8Plan plan_i8(int M, int N, int Kp) {
   for (const I8Cost& c : kI8Costs) {
     const long long mt = (M + c.bm - 1) / c.bm, nt = (N + c.bn - 1) / c.bn;
     if (mt > 65535) continue;  // (the grid's second dimension)
-    if ((M + c.bm - 1) / c.bm > 65535) continue;  // (a launch's tiles in y)
     for (const int S : {1, 2, 3, 4, 6, 8}) {
       if (S > 1 && (c.wide || S > lines)) break;
       const int per = (lines + S - 1) / S, used = (lines + per - 1) / per;
@@ -586,6 +585,10 @@ I8Plan plan_i8(int M, int N, int Kp) {
     }
   }
   return best;
+}
+
+I8Plan plan_i8(int M, int N, int Kp) {
+  return last_plan<I8Plan>({M, N, Kp}, [&] { return choose_i8(M, N, Kp); });
 }
 
 void launch_quant8(int dtype, const void* x, int x_rows, const int* rows, int M, int K, int8_t* q, float* scale, hipStream_t st) {
