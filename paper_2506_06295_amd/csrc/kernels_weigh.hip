@@ -500,7 +500,8 @@ __global__ __launch_bounds__(256, D == 256 && sizeof(T) == 4 ? 1 : 2) void k_wei
 }
 
 // Up to 128 KB keys: the eight wavefronts of a workgroup hold them all, 16 KB each, and walk a share of the head's rows 16 at a time.
-// Scores stay in registers while the wavefronts exchange their maxima and sums; no second pass, no z.
+// Scores stay in registers while the wavefronts exchange their maxima and sums; no second pass.  Bound by a wavefront's instructions:
+// KB follows the keys in steps of two (768 keys by eight wavefronts of 96 11.1 us with the sum, by six of 128 12.7, of 64 rows x 32 heads).
 template <typename F, typename T, int D, int KB>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_weigh_short(const T* __restrict__ q, WeighShape s, CacheView k,
                                                                                          Keys keys, float* __restrict__ part) {
@@ -630,7 +631,7 @@ WeighPlan plan_weigh(int dtype, int format, int B, int Mq, int n, int H_q, int H
   const int most = short_blocks(format == 0, dtype == 0, d_h);
   if (n <= 128 * most) {
     p.brief = true;
-    p.KB = n <= 256 || most == 2 ? 2 : n <= 512 || most == 4 ? 4 : 8;
+    p.KB = n <= 256 || most == 2 ? 2 : n <= 512 || most == 4 ? 4 : n <= 768 ? 6 : 8;
     const int rt = (s.NR + 15) / 16;
     // A workgroup per CU, two where the registers leave room for more: 3 % from the quickest share count on average (40 shapes; half as many
     // workgroups 8 %, in the worst 2 times as long: a tile of rows is a chain of loads, products, two exchanges and a barrier)
@@ -695,6 +696,7 @@ void launch_attention_weights(const WeighPlan& p, int dtype, int format, const v
         if (p.KB == 4) hipLaunchKernelGGL((k_weigh_short<F, T, D, 4>), grid, dim3(512), 0, st, qt, s, k, keys, part);
       }
       if constexpr (most >= 8) {
+        if (p.KB == 6) hipLaunchKernelGGL((k_weigh_short<F, T, D, 6>), grid, dim3(512), 0, st, qt, s, k, keys, part);
         if (p.KB == 8) hipLaunchKernelGGL((k_weigh_short<F, T, D, 8>), grid, dim3(512), 0, st, qt, s, k, keys, part);
       }
       return;

@@ -54,21 +54,23 @@ def test_attention_kernels(dtype, B, Mq, n, H_q, H_kv, d_h, rows, waves, kind, w
 
 WEIGH = [  # dtype, format, B, Mq, n, H_q, H_kv, d_h -> keys of a wavefront, ranges (0: one launch; 2: several), rows, several shares
     ("bf16", "bf16", 1, 40, 200, 2, 2, 64, 32, 0, 16, 1), ("bf16", "bf16", 1, 24, 306, 1, 1, 64, 64, 0, 16, 1),
-    ("bf16", "bf16", 1, 9, 538, 1, 1, 64, 128, 0, 16, 0), ("bf16", "bf16", 1, 5, 1377, 1, 1, 64, 64, 2, 16, 0),
+    ("bf16", "bf16", 1, 9, 538, 1, 1, 64, 96, 0, 16, 0), ("bf16", "bf16", 1, 5, 1377, 1, 1, 64, 64, 2, 16, 0),
     ("bf16", "bf16", 1, 39, 1351, 1, 1, 64, 64, 2, 64, 0), ("bf16", "bf16", 1, 1056, 1029, 8, 4, 64, 64, 1, 64, 1),
-    ("bf16", "bf16", 1, 18, 601, 1, 1, 128, 128, 0, 16, 1), ("bf16", "bf16", 1, 1, 1038, 1, 1, 128, 64, 2, 16, 0),
+    ("bf16", "bf16", 1, 18, 601, 1, 1, 128, 96, 0, 16, 1), ("bf16", "bf16", 1, 1, 1038, 1, 1, 128, 64, 2, 16, 0),
     ("bf16", "bf16", 1, 3, 1040, 7, 1, 128, 64, 2, 32, 0), ("bf16", "bf16", 1, 22, 1081, 2, 1, 128, 64, 2, 64, 1),
     ("bf16", "bf16", 4, 529, 1059, 4, 4, 128, 64, 1, 64, 1), ("bf16", "bf16", 1, 19, 265, 1, 1, 256, 64, 0, 16, 1),
     ("bf16", "bf16", 1, 3, 525, 7, 1, 256, 32, 2, 16, 1), ("bf16", "bf16", 4, 37, 523, 14, 2, 256, 32, 1, 16, 1),
-    ("bf16", "kv4", 1, 17, 621, 1, 1, 64, 128, 0, 16, 1), ("bf16", "kv4", 1, 26, 1185, 1, 1, 64, 64, 2, 32, 0),
-    ("bf16", "kv4", 2, 264, 1042, 16, 8, 64, 64, 1, 64, 1), ("bf16", "kv4", 1, 17, 526, 1, 1, 128, 128, 0, 16, 1),
+    ("bf16", "kv4", 1, 17, 621, 1, 1, 64, 96, 0, 16, 1), ("bf16", "kv4", 1, 26, 1185, 1, 1, 64, 64, 2, 32, 0),
+    ("bf16", "kv4", 2, 264, 1042, 16, 8, 64, 64, 1, 64, 1), ("bf16", "kv4", 1, 17, 526, 1, 1, 128, 96, 0, 16, 1),
     ("bf16", "kv4", 1, 17, 1083, 2, 1, 128, 64, 2, 64, 1), ("bf16", "kv4", 1, 627, 1027, 14, 2, 128, 64, 1, 64, 1),
     ("bf16", "kv4", 1, 12, 557, 2, 1, 256, 32, 2, 16, 1), ("f32", "f32", 1, 19, 933, 1, 1, 64, 128, 0, 16, 1),
     ("f32", "f32", 1, 22, 1376, 2, 1, 64, 32, 2, 16, 1), ("f32", "f32", 1, 10, 279, 2, 1, 128, 64, 0, 16, 1),
     ("f32", "f32", 1, 1050, 533, 2, 2, 128, 32, 1, 16, 1), ("f32", "f32", 1, 25, 305, 1, 1, 256, 32, 1, 16, 1),
-    ("f32", "f32", 1, 3, 604, 7, 1, 256, 32, 2, 16, 1), ("f32", "kv4", 1, 4, 572, 7, 1, 64, 128, 0, 16, 1),
+    ("f32", "f32", 1, 3, 604, 7, 1, 256, 32, 2, 16, 1), ("f32", "kv4", 1, 4, 572, 7, 1, 64, 96, 0, 16, 1),
     ("f32", "kv4", 1, 34, 1081, 1, 1, 64, 64, 2, 16, 1), ("f32", "kv4", 1, 9, 308, 2, 1, 128, 64, 0, 16, 1),
     ("f32", "kv4", 1, 12, 576, 2, 1, 128, 64, 2, 16, 1), ("f32", "kv4", 1, 18, 363, 1, 1, 256, 32, 1, 16, 1),
+    ("bf16", "bf16", 1, 9, 857, 1, 1, 64, 128, 0, 16, 0), ("bf16", "bf16", 1, 18, 902, 1, 1, 128, 128, 0, 16, 1), ("bf16", "kv4", 1, 17, 1001, 1, 1, 64, 128, 0, 16, 1),
+    ("bf16", "kv4", 1, 17, 771, 1, 1, 128, 128, 0, 16, 1), ("f32", "kv4", 1, 4, 969, 7, 1, 64, 128, 0, 16, 1), ("f32", "f32", 1, 21, 767, 1, 1, 64, 96, 0, 16, 1),
 ]
 
 
