@@ -27,7 +27,8 @@ __global__ __launch_bounds__(64 * W) void k_evict(const float* __restrict__ acc,
                                                   float* __restrict__ acc_out) {
   constexpr int kThreads = 64 * W;
   __shared__ __attribute__((aligned(16))) uint32_t hist[256 * 64];
-  __shared__ int bins[256], found[3], counts[2][W];
+  __shared__ __attribute__((aligned(16))) int bins[256];  // (read as int4)
+  __shared__ int found[3], counts[2][W];
   const int b = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   constexpr int kBatch = 16;  // trips whose loads go out together where not all do
   const int trips = KPT > 0 ? KPT : (keys.n + kBatch * kThreads - 1) / (kBatch * kThreads) * kBatch;
