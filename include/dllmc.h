@@ -404,7 +404,8 @@ int dllmc_op_attention(int32_t dtype, const void* q, int32_t B, int32_t Mq, cons
  * eviction of positions by it, and linear maps in 8-bit integers, whose weights are half the bytes an adaptive step streams.
  * As with the other single operations all memory is the caller's, nothing is allocated, cleared by the runtime or
  * waited for (every call can be captured into a graph), and calls that share scratch must be ordered.  Results must lie
- * apart from the operands (DLLMC_EINVAL) unless said otherwise.  Data pointers are 16-byte aligned, int32 and float32 lists 4-byte.
+ * apart from the operands (DLLMC_EINVAL) unless said otherwise, and so must the bytes of scratch that a call needs, from results
+ * too.  Data pointers are 16-byte aligned, int32 and float32 lists 4-byte.
  *
  * 4-bit cache tensor of cache_rows rows, H heads of d_h elements (d_h a multiple of 32, H * d_h <= 65536): dllmc_kv4_bytes()
  * bytes (0: invalid).  Codes [H][cache_rows][d_h / 2], element 2t of a row in the low half of byte t; at the next multiple of

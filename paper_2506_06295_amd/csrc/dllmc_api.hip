@@ -1253,6 +1253,9 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
   for (const auto& i : in)
     if (i.n && (!apart(out, qb, i.p, i.n) || (lse && !apart(lse, rows * 4, i.p, i.n)))) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  if (need && (!apart(scratch, need, out, qb) || (lse && !apart(scratch, need, lse, rows * 4)))) return DLLMC_EINVAL;
+  for (const auto& i : in)
+    if (need && i.n && !apart(scratch, need, i.p, i.n)) return DLLMC_EINVAL;
   (void)hipGetLastError();
   launch_attention_kv4(plan, dtype, q, Mq, cache_view(DLLMC_KV4, k_cache, cache_rows, H_kv, d_h),
                        cache_view(DLLMC_KV4, v_cache, cache_rows, H_kv, d_h), Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, out,
@@ -1287,6 +1290,9 @@ int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* 
   for (const auto& i : in)
     if (i.n && !apart(acc_out, ob, i.p, i.n)) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  if (!apart(scratch, need, acc_out, ob)) return DLLMC_EINVAL;  // (partial sums: there is always some)
+  for (const auto& i : in)
+    if (i.n && !apart(scratch, need, i.p, i.n)) return DLLMC_EINVAL;
   (void)hipGetLastError();
   launch_attention_weights(plan, dtype, cache_format, q, B, Mq, cache_view(cache_format, k_cache, cache_rows, H_kv, d_h),
                            Keys{lens, row_map, n, cache_rows}, H_q, H_kv, d_h, lse, acc_in, acc_out, scratch,
@@ -1410,10 +1416,14 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
   const I8Plan plan = plan_i8(M, N, static_cast<int>(kp));
   const size_t need = linear_i8_scratch_bytes(plan, M, N);
   const size_t ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
-  if (!apart(out, ob, a, M * kp) || !apart(out, ob, w, N * kp) || !apart(out, ob, a_scale, static_cast<size_t>(M) * 4) ||
-      !apart(out, ob, w_scale, static_cast<size_t>(N) * 4))
-    return DLLMC_EINVAL;
+  const struct { const void* p; size_t n; } in[] = {{a, M * kp}, {w, N * kp}, {a_scale, static_cast<size_t>(M) * 4},
+                                                    {w_scale, static_cast<size_t>(N) * 4}};
+  for (const auto& i : in)
+    if (!apart(out, ob, i.p, i.n)) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  if (need && !apart(scratch, need, out, ob)) return DLLMC_EINVAL;
+  for (const auto& i : in)
+    if (need && !apart(scratch, need, i.p, i.n)) return DLLMC_EINVAL;
   (void)hipGetLastError();
   launch_linear_i8(plan, dtype, a, a_scale, M, w, w_scale, N, K, out, scratch, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
