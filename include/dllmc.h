@@ -430,7 +430,7 @@ int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int3
  *
  * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
  * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without
- * keys gets zeros and an lse of minus infinity.  scratch: at least dllmc_op_attention_kv4_scratch_bytes() bytes, which may
+ * keys gets zeros and an lse of minus infinity, and so does a row whose every score is minus infinity.  scratch: at least dllmc_op_attention_kv4_scratch_bytes() bytes, which may
  * be 0. */
 size_t dllmc_op_attention_kv4_scratch_bytes(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv,
                                             int32_t d_h);
@@ -440,9 +440,9 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
                            void* hip_stream);
 /* Attention weight of every cached position: acc_out[b][j] = acc_in[b][j] (0 if NULL; may be acc_out) + the sum over the Mq
  * queries and H_q heads of their softmax probabilities, float32 [B, n], B * n * H_kv <= 2^30; positions that are not there get
- * nothing.  k_cache: [cache_rows, H_kv * d_h] in the dtype of q (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what
- * dllmc_op_attention_kv4 gave for these operands, or NULL (then it is worked out first: beyond 1024 keys at most they are read
- * twice).  Bit-reproducible. */
+ * nothing, rows whose every score is minus infinity give nothing.  k_cache: [cache_rows, H_kv * d_h] in the dtype of q
+ * (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what dllmc_op_attention_kv4 gave for these operands, or NULL
+ * (then it is worked out first: beyond 1024 keys at most they are read twice).  Bit-reproducible. */
 size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n,
                                                 int32_t H_q, int32_t H_kv, int32_t d_h);
 int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* q, int32_t B, int32_t Mq,

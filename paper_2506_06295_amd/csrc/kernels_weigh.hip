@@ -210,6 +210,9 @@ template <typename Op> __device__ __forceinline__ void turn_keys16(typename Op::
   }
 }
 
+// 1 / l of a row; 0 where the sum is empty (no key, or every score minus infinity): such a row weighs nothing
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
 // (m, l) of 16 QB rows over a range of keys, base 2, or m and 1 / l where the range is all of them; the eight wavefronts deal the range's blocks
 // of 32 keys, the next one in flight.  Bound by vector instructions: 4.6 a score, one per 6 cycles with two wavefronts per SIMD (an
 // exponential 12); with four of them, queries read from LDS again for every block, the same.  512 rows x 4608 keys x 32 heads in 4 bits
@@ -336,7 +339,7 @@ __global__ __launch_bounds__(64 * kSW) __attribute__((amdgpu_waves_per_eu(2))) v
     const size_t w = row_of(s, b, h, r0 + threadIdx.x);
     if (s.KS == 1) {
       m_out[w] = v.x;
-      il_out[w] = 1.f / v.y;
+      il_out[w] = reciprocal(v.y);
     } else {
       ml[w * s.KS + range] = v;
     }
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(256) void k_weigh_join(const float2* __restrict__ m
     m = M;
   }
   m_out[w] = m;
-  il_out[w] = 1.f / l;
+  il_out[w] = reciprocal(l);
 }
 
 // 16 KB column sums of a wavefront leave for part[j], zero where there is no key; `there`: keys of each 16
@@ -476,7 +479,8 @@ __device__ __forceinline__ void weigh_cols_body(const T* __restrict__ q, const W
         const float* row = reinterpret_cast<const float*>(&lds[NS * St::kVecs + (slot * 4 + wave) * 32]) + r;
         float mr = row[0] * mul;
         const float ir = il != nullptr ? row[64] : 1.f;
-        if (t * St::kRows + r >= s.NR) mr = INFINITY;  // rows past the last one weigh nothing
+        // rows past the last one weigh nothing, nor do those whose every score is minus infinity (which minus itself would be NaN)
+        if (t * St::kRows + r >= s.NR || mr == -INFINITY) mr = INFINITY;
         typename Op::Query qf;
         Op::query_pieces([&](int c) { return lds[slot * St::kVecs + r * kChunks + (c ^ (r % kMix))]; }, lg, qf);
 #pragma unroll
