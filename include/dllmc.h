@@ -441,8 +441,9 @@ int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, 
 /* Attention weight of every cached position: acc_out[b][j] = acc_in[b][j] (0 if NULL; may be acc_out) + the sum over the Mq
  * queries and H_q heads of their softmax probabilities, float32 [B, n], B * n * H_kv <= 2^30; positions that are not there get
  * nothing, rows whose every score is minus infinity give nothing.  k_cache: [cache_rows, H_kv * d_h] in the dtype of q
- * (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: what dllmc_op_attention_kv4 gave for these operands, or NULL
- * (then it is worked out first: beyond 1024 keys at most they are read twice).  Bit-reproducible. */
+ * (cache_format = dtype), or a 4-bit tensor (DLLMC_KV4).  lse: the rows' log-sum-exps over these operands, as
+ * dllmc_op_attention_kv4 gives them for a 4-bit cache (for another cache the caller has them from elsewhere), or NULL: then they are
+ * worked out first, and beyond 1024 keys at most those are read twice (up to there lse is not looked at).  Bit-reproducible. */
 size_t dllmc_op_attention_weights_scratch_bytes(int32_t dtype, int32_t cache_format, int32_t B, int32_t Mq, int32_t n,
                                                 int32_t H_q, int32_t H_kv, int32_t d_h);
 int dllmc_op_attention_weights(int32_t dtype, int32_t cache_format, const void* q, int32_t B, int32_t Mq,

@@ -656,7 +656,8 @@ def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache
                          row_map: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                          acc: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """float32 [B, n]: acc (0 if None) plus the attention weight that q gives to every cached position.  cache_format: the
-    dtype, or "kv4".  lse: of op_attention_kv4 over the same operands, if there is one.  out: where it goes (may be acc)."""
+    dtype, or "kv4".  lse: the rows' log-sum-exps over these operands (of op_attention_kv4 for "kv4"), if there are any.  out: where it
+    goes (may be acc)."""
     code, tdt = _DTYPES[dtype]
     fmt = _format(cache_format)
     B, Mq = q.shape[:2]
