@@ -610,7 +610,9 @@ __global__ __launch_bounds__(64 * WV, 2) void k_attend_tile(const bf16_t* __rest
 }
 
 // ---- ranges joined -------------------------------------------------------------------------------------
-// One wavefront per row of the items that were cut (`rows` of an item): its ranges in order.
+// One wavefront per row of the items that were cut (`rows` of an item): its ranges in order, each loaded when the one before it has
+// been added (the compiler does not unroll a loop of unknown length with a shuffle in it).  Bound by those trips to memory, behind that
+// for the maxima and sums: 4 us with two ranges.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_attend_merge(const float* __restrict__ part, const float2* __restrict__ part_ml, AttendShape s,
                                                       int rows, T* __restrict__ out, float* __restrict__ lse) {
@@ -630,7 +632,6 @@ __global__ __launch_bounds__(256) void k_attend_merge(const float* __restrict__ 
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   const float* p = part + static_cast<size_t>(at) * s.KS * D + lane * E;
-#pragma unroll 8
   for (int i = 0; i < s.KS; ++i) {
     const float fk = __shfl(f, i, 64);
 #pragma unroll
