@@ -592,6 +592,12 @@ def _need_cache(name: str, fmt: str, t: torch.Tensor, cache_rows: int, H: int, d
     return _need(name, t, _DTYPES[fmt][1], (cache_rows, H * d_h), device)
 
 
+def _need_positions(n: int) -> None:
+    # (no tensor's shape need say n, and the calls take 32 bits of it)
+    if not 0 < n < 1 << 31:
+        raise DllmcError(f"n: no {n} positions")
+
+
 def _format(fmt: str) -> int:
     return DLLMC_KV4 if fmt == "kv4" else _DTYPES[fmt][0]
 
@@ -599,7 +605,7 @@ def _format(fmt: str) -> int:
 @functools.lru_cache(maxsize=1024)
 def kv4_bytes(cache_rows: int, H: int, d_h: int) -> int:
     """Bytes of a 4-bit cache tensor (a uint8 tensor of that size holds it)."""
-    n = lib().dllmc_kv4_bytes(cache_rows, H, d_h)
+    n = lib().dllmc_kv4_bytes(cache_rows, H, d_h) if all(0 < v < 1 << 31 for v in (cache_rows, H, d_h)) else 0  # (of 32 bits)
     if n == 0:
         raise DllmcError(f"dllmc_kv4_bytes: no 4-bit tensor of {cache_rows} rows, {H} heads of {d_h}")
     return n
@@ -638,6 +644,7 @@ def op_attention_kv4(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache
     code, tdt = _DTYPES[dtype]
     B, Mq = q.shape[:2]
     dev = _device("q", q)
+    _need_positions(n)
     qp = _need("q", q, tdt, (B, Mq, H_q * d_h), dev)
     kp = _need_cache("k_cache", "kv4", k_cache, cache_rows, H_kv, d_h, dev)
     vp = _need_cache("v_cache", "kv4", v_cache, cache_rows, H_kv, d_h, dev)
@@ -662,6 +669,7 @@ def op_attention_weights(dtype: str, cache_format: str, q: torch.Tensor, k_cache
     fmt = _format(cache_format)
     B, Mq = q.shape[:2]
     dev = _device("q", q)
+    _need_positions(n)
     qp = _need("q", q, tdt, (B, Mq, H_q * d_h), dev)
     kp = _need_cache("k_cache", cache_format, k_cache, cache_rows, H_kv, d_h, dev)
     lp, rp = _need("lens", lens, torch.int32, (B,), dev), _need("row_map", row_map, torch.int32, (B, n), dev)
@@ -682,9 +690,13 @@ def op_evict(acc: torch.Tensor, keep: int, cache_rows: int, first: int = 0, last
     dllmc_op_evict."""
     B, n = acc.shape
     dev = _device("acc", acc)
+    if not (1 <= keep <= n and first >= 0 and last >= 0 and first + last <= keep and 1 <= cache_rows < 1 << 31):
+        # (what is allocated goes by keep, and the call takes 32 bits of each)
+        raise DllmcError(f"op_evict: cannot keep {keep} of {n} positions, the first {first} and last {last} among them, of a cache of "
+                         f"{cache_rows} rows")
     ap = _need("acc", acc, torch.float32, (B, n), dev)
     lp, rp = _need("lens", lens, torch.int32, (B,), dev), _need("row_map", row_map, torch.int32, (B, n), dev)
-    left = acc.new_empty((B, max(keep, 0)))
+    left = acc.new_empty((B, keep))
     kept = torch.empty_like(left, dtype=torch.int32)
     kept_rows, new_lens = torch.empty_like(kept), acc.new_empty(B, dtype=torch.int32)
     _check(lib().dllmc_op_evict(ap, B, n, lp, rp, cache_rows, keep, first, last, kept.data_ptr(), kept_rows.data_ptr(),
@@ -712,7 +724,7 @@ def op_compact(cache_format: str, rows: torch.Tensor, src_rows: int, H: int, d_h
 @functools.lru_cache(maxsize=1024)
 def i8_row_bytes(K: int) -> int:
     """Bytes of a row of K 8-bit integers: K rounded up to 128."""
-    n = lib().dllmc_i8_row_bytes(K)
+    n = lib().dllmc_i8_row_bytes(K) if 0 < K < 1 << 31 else 0  # (of 32 bits)
     if n == 0:
         raise DllmcError(f"dllmc_i8_row_bytes: no 8-bit rows of {K}")
     return n
