@@ -546,6 +546,12 @@ def op_attention(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
                  H_q: int, H_kv: int, d_h: int, split_keys: bool = True) -> torch.Tensor:
     B, Mq, _ = q.shape
     n = k_cache.shape[1]
+    # (the library takes sizes, not tensors: what is smaller than they say would be read past its end)
+    for name, t, numel in (("q", q, B * Mq * H_q * d_h), ("k_cache", k_cache, B * n * H_kv * d_h), ("v_cache", v_cache, B * n * H_kv * d_h)):
+        if t.numel() != numel or t.dtype is not _DTYPES[dtype][1] or not t.is_contiguous():
+            raise DllmcError(f"op_attention: {name} has to be a contiguous {dtype} tensor of {numel} elements, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_cuda:
+            raise DllmcError(f"op_attention: {name} has to be on the device")
     out = torch.empty_like(q)
     scratch = None
     if split_keys:
