@@ -550,8 +550,8 @@ def op_attention(dtype: str, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     for name, t, numel in (("q", q, B * Mq * H_q * d_h), ("k_cache", k_cache, B * n * H_kv * d_h), ("v_cache", v_cache, B * n * H_kv * d_h)):
         if t.numel() != numel or t.dtype is not _DTYPES[dtype][1] or not t.is_contiguous():
             raise DllmcError(f"op_attention: {name} has to be a contiguous {dtype} tensor of {numel} elements, got {t.dtype} {tuple(t.shape)}")
-        if not t.is_cuda:
-            raise DllmcError(f"op_attention: {name} has to be on the device")
+    if not (q.is_cuda and k_cache.is_cuda and v_cache.is_cuda):
+        raise DllmcError("op_attention: the tensors have to be on the device")
     out = torch.empty_like(q)
     scratch = None
     if split_keys:
