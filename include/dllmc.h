@@ -407,8 +407,9 @@ int dllmc_op_attention(int32_t dtype, const void* q, int32_t B, int32_t Mq, cons
  * apart from the operands (DLLMC_EINVAL) unless said otherwise, and so must the bytes of scratch that a call needs, from results
  * too.  Data pointers are 16-byte aligned, int32 and float32 lists 4-byte.
  *
- * 4-bit cache tensor of cache_rows rows, H heads of d_h elements (d_h a multiple of 32, H * d_h <= 65536): dllmc_kv4_bytes()
- * bytes (0: invalid).  Codes [H][cache_rows][d_h / 2], element 2t of a row in the low half of byte t; at the next multiple of
+ * 4-bit cache tensor of cache_rows rows (a cache of any format has at most 2^24, and so has a call's M), H heads of d_h elements
+ * (d_h a multiple of 32, H * d_h <= 65536): dllmc_kv4_bytes() bytes (0: invalid).  Codes [H][cache_rows][d_h / 2], element 2t of
+ * a row in the low half of byte t; at the next multiple of
  * 256 bytes scale bytes [H][cache_rows][d_h / 32].  A block of 32 elements has one scale s that stands for 2^(s - 127): the
  * smallest power of two, of 2^-125 .. 2^125, with max |x| <= 6 * 2^(s - 127).  A code is a sign and the index of one of 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6, the nearest to x / 2^(s - 127) (ties to the even index, beyond 6: 6).  s = 255: the block held an infinity
@@ -425,8 +426,8 @@ int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int3
 /* Cached keys of the operations below: sequence b has the positions j < lens[b] (n if lens is NULL; values outside [0, n] count
  * as the nearest of the two), position j in cache row row_map[b * n + j] (b * n + j if row_map is NULL).  A position whose entry is
  * no row of the cache is not there.  What lies in rows and positions that are not there has no influence whatever it
- * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements; B <= 65536, B * n <= 2^24 positions, fewer than 2^23
- * rows B * Mq * H_q.
+ * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements, H_q * d_h <= 65536; B <= 65536, B * n <= 2^24
+ * positions, fewer than 2^23 rows B * Mq * H_q.
  *
  * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
  * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without
@@ -466,8 +467,8 @@ int dllmc_op_compact(int32_t cache_format, const int32_t* rows, int32_t M, int32
 /* Rows in 8-bit integers: dllmc_i8_row_bytes(K) bytes each, K rounded up to 128 (K <= 131072; 0: invalid), zeros behind the K-th.
  * q[i][k] = the integer nearest to the float32 product x[r][k] * f, ties to even, f = 127 * (1 / max|x[r]|), scale[i] =
  * max|x[r]| / 127, r = row_idx[i] (i if NULL), x [x_rows, K], aligned to its elements.  A row whose maximum is below 2^-118, and an
- * r outside [0, x_rows), becomes zeros with scale 0; a row with an infinity or NaN zeros with scale NaN.  For weights (rows =
- * output channels) as for activations (rows = tokens). */
+ * r outside [0, x_rows), becomes zeros with scale 0; a row with an infinity or NaN zeros with scale NaN.  M < 2^24.  For weights
+ * (rows = output channels) as for activations (rows = tokens). */
 size_t dllmc_i8_row_bytes(int32_t K);
 int dllmc_op_quant8(int32_t dtype, const void* x, int32_t x_rows, const int32_t* row_idx, int32_t M, int32_t K, int8_t* q, float* scale,
                     void* hip_stream);

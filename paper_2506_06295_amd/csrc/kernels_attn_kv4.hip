@@ -21,7 +21,7 @@ typedef short v8s __attribute__((ext_vector_type(8)));
 // the elements to the contraction will do that the queries share; this one makes a load of 16 keys one run of memory).  V: piece
 // t 64 + lane of 32 elements, of key piece / (D / 32).
 template <int D> struct KeyBlock {
-  static constexpr int kW = D / 32, kV = D / 64, kKS = D == 256 ? 2 : 1;
+  static constexpr int kW = D / 32, kV = D / 64;
   uint32_t k[2][kW];
   uint32_t ks[2];
   uint4 v[kV];
@@ -649,7 +649,9 @@ __global__ __launch_bounds__(256) void k_attend_merge(const float* __restrict__ 
 // 4608 rows, 96 to 16384 keys, 1 to 16 sequences; the choices are 1.3 % from the quickest on average.  Us (heads of 128): one row x 4608
 // keys x 32 heads 12.5, 51 rows 19 to 21 (by what the caches hold), 16 sequences x 1 row x 4099 keys x 28 / 4 heads in pages 16.7, 4608 rows
 // x 4608 keys x 32 heads 448 (0.78 PFLOP/s, 1.17 with the remainders' products): two and a quarter rounds of 256 workgroups, of which the
-// quarter is cut in four.
+// quarter is cut in four.  Float32 and heads of 256 have one kernel, 16 rows by four wavefronts: 51 rows x 4608 keys x 32 heads in float32
+// 25.5, 576 rows x 28 / 4 heads 127, 4608 rows x 32 heads 986 (773 at the bf16 rate of its six products); 16 heads of 256 in bf16: one row 15.1, 51
+// rows 29, 512 rows 104, 4608 rows 823 (386): every 16 rows expand all keys again.
 struct AttendCost { int d, f32, rows, waves, groups; double start, round, block, share, mb, cut, part, range; };
 constexpr AttendCost kAttendCosts[] = {
     {64, 1, 16, 4, 5, 2.78, 0.56, 0.258, 0.406, 0, 2.68, 0.521, 0.268},

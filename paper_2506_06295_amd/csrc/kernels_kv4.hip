@@ -1,4 +1,4 @@
-// K/V cache tensors held in 4 bits, and the attention that reads them.
+// K/V cache tensors held in 4 bits: rows in and out.
 //
 // A block is 32 neighbouring elements of a head: codes of 4 bits (sign, and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) times one power of
 // two, the smallest that holds the block's largest magnitude.  What a code stands for is exact in bf16 (two significant bits,
