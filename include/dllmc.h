@@ -427,12 +427,14 @@ int dllmc_op_kv4_load(int32_t dtype, const void* cache, int32_t cache_rows, int3
  * as the nearest of the two), position j in cache row row_map[b * n + j] (b * n + j if row_map is NULL).  A position whose entry is
  * no row of the cache is not there.  What lies in rows and positions that are not there has no influence whatever it
  * is.  lens and row_map are device int32 lists; heads of 64, 128 or 256 elements, H_q * d_h <= 65536; B <= 65536, B * n <= 2^24
- * positions, fewer than 2^23 rows B * Mq * H_q.
+ * positions, fewer than 2^23 rows B * Mq * H_q.  Finite scaled scores are to stay below 2^30 in magnitude: beyond, where float32 is
+ * too coarse for the exponents that are taken from it, a row (and the weights of its sequence) may become NaN.
  *
  * Attention of Mq queries per sequence over a 4-bit cache, as dllmc_op_attention otherwise: q, out [B, Mq, H_q * d_h].  lse
  * (may be NULL): float32 [B, Mq, H_q], the logarithm of the sum of exponentials of the scaled scores.  A sequence without
- * keys gets zeros and an lse of minus infinity, and so does a row whose every score is minus infinity.  scratch: at least dllmc_op_attention_kv4_scratch_bytes() bytes, which may
- * be 0. */
+ * keys gets zeros and an lse of minus infinity, and so does a row whose every score is minus infinity.  An element of a float32
+ * query that bf16 has as an infinity (3.3962e38 and beyond) makes its row NaN over a 4-bit cache.  scratch: at least
+ * dllmc_op_attention_kv4_scratch_bytes() bytes, which may be 0. */
 size_t dllmc_op_attention_kv4_scratch_bytes(int32_t dtype, int32_t B, int32_t Mq, int32_t n, int32_t H_q, int32_t H_kv,
                                             int32_t d_h);
 int dllmc_op_attention_kv4(int32_t dtype, const void* q, int32_t B, int32_t Mq, const void* k_cache, const void* v_cache,

@@ -120,7 +120,7 @@ template <typename T> struct Parts;  // bf16 parts of a query element and of a p
 template <> struct Parts<bf16_t> { static constexpr int kQ = 1, kP = 2; };
 template <> struct Parts<float> { static constexpr int kQ = 3, kP = 3; };
 
-// Eight query elements as bf16 parts: x = part 0 + part 1 + part 2, each what is left rounded.
+// Eight query elements as bf16 parts: x = part 0 + part 1 + part 2, each what is left rounded (what rounds to an infinity leaves NaN).
 __device__ __forceinline__ void load_query(const bf16_t* p, bf16x8 (&f)[1]) {
   f[0] = *reinterpret_cast<const bf16x8*>(p);
 }

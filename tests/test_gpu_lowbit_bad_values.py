@@ -137,3 +137,70 @@ def test_attention_with_nan(dtype, Mq, n, H_q, H_kv, d_h, what):
             assert torch.equal(lse, want_lse)
         else:
             assert lse[spoilt[..., 0]].isnan().all() and torch.equal(lse[~spoilt[..., 0]], want_lse[~spoilt[..., 0]])
+
+
+@pytest.mark.parametrize("Mq,n", [(3, 90), (20, 3000)])
+@pytest.mark.parametrize("value", [float("-inf"), float("inf"), 3.4028234e38, 3.3961e38])
+def test_float32_queries_at_the_end_of_the_range(Mq, n, value):
+    """Over 4 bits: what bf16 has as an infinity makes its row NaN; other rows are as they were, whatever the score (2^107 here, far
+    beyond what the header allows)."""
+    c = Case(21, "f32", 1, Mq, n, 2, 1, 128)
+    c.k = (np.sign(c.k) * 2.0 ** -20).astype(np.float32)
+    q, k, v, _ = c.device("kv4")
+    args = (c.rows, n, 2, 1, 128)
+    want, want_lse = L.op_attention_kv4("f32", q, k, v, *args, with_lse=True)
+    row, rest = (0, Mq // 2, 1), torch.ones(1, Mq, 2, dtype=torch.bool, device="cuda")
+    rest[row] = False
+    q[0, Mq // 2, 128:] = 0.0
+    q[0, Mq // 2, 130] = value
+    got, lse = L.op_attention_kv4("f32", q, k, v, *args, with_lse=True)
+    assert torch.equal(got.view(1, Mq, 2, 128)[rest], want.view(1, Mq, 2, 128)[rest]) and torch.equal(lse[rest], want_lse[rest])
+    if value != 3.3961e38:
+        assert got.view(1, Mq, 2, 128)[row].isnan().all() and lse[row].isnan()
+        assert weights(c, "kv4", q, k).isnan().all()
+
+
+@pytest.mark.parametrize("Mq,n", [(3, 90), (20, 3000)])
+def test_float32_queries_below_the_end_of_the_range(Mq, n):
+    """The largest element that bf16 does not have as an infinity, over keys that make scores of +-22.6 of it: the keys of its sign share the
+    row, the others have e^-45 of their weight."""
+    c = Case(22, "f32", 1, Mq, n, 2, 1, 128)
+    c.k = (np.sign(c.k) * 2.0 ** -120).astype(np.float32)
+    c.q[0, Mq // 2, 1] = 0.0
+    c.q[0, Mq // 2, 1, 2] = 3.3961e38
+    check = c.values("kv4", c.k)
+    assert np.array_equal(check.reshape(c.k.shape), c.k)          # a power of two is held exactly
+    q, k, v, _ = c.device("kv4")
+    got, lse = L.op_attention_kv4("f32", q, k, v, c.rows, n, 2, 1, 128, with_lse=True)
+    up = c.k[:, 2] > 0
+    score = 3.3961e38 * 2.0 ** -120 / np.sqrt(128)
+    # scores off by 3 * 2^-24 of themselves, the same for all; sums of n terms
+    assert abs(float(lse[0, Mq // 2, 1]) - (score + np.log(up.sum()))) <= (score + np.log(n)) * 2.0 ** -21 + n * 2.0 ** -24
+    values = c.values("kv4", c.v)[:, 0]
+    err = np.abs(got.view(1, Mq, 2, 128)[0, Mq // 2, 1].double().cpu().numpy() - values[up].mean(0))
+    assert (err <= np.abs(values).max() * (n * 2.0 ** -22 + 2.0 ** -20)).all()
+    w = weights(c, "kv4", q, k).double().cpu().numpy()[0]
+    rest = torch.arange(Mq, device="cuda") != Mq // 2
+    assert np.isfinite(w).all() and abs(w.sum() - 2 * Mq) <= 2 * Mq * n * 2.0 ** -22 and bool(got[0, rest].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("Mq,n,d_h", [(3, 90, 128), (20, 3000, 128), (200, 1100, 64), (5, 700, 256)])
+def test_the_largest_scores(dtype, fmt, Mq, n, d_h):
+    """Scores of both signs to just below 2^30: everything finite, every row's weights sum to one, its log-sum-exp is its largest score."""
+    c = Case(23, dtype, 1, Mq, n, 2, 1, d_h)
+    c.q[:] = 0.0
+    c.q[..., 3] = R.grid(c.r.uniform(0.25, 1.0, c.q.shape[:3]) * c.r.choice([-1.0, 1.0], c.q.shape[:3]) * 2.0 ** 20 * np.sqrt(d_h), dtype)
+    c.k = R.grid(c.r.uniform(-1.0, 1.0, c.k.shape) * 2.0 ** 9.98, dtype)
+    q, k, v, _ = c.device(fmt)
+    held = c.values(fmt, c.k)[:, 0, 3]
+    scores = c.q[0, :, :, 3, None].astype(np.float64) * held / np.sqrt(d_h)      # [Mq, H_q, n]
+    assert 2.0 ** 29 < np.abs(scores).max() < 2.0 ** 30
+    w = weights(c, fmt, q, k).double().cpu().numpy()[0]
+    assert np.isfinite(w).all() and (w >= 0).all()
+    assert abs(w.sum() - 2 * Mq) <= 2 * Mq * (n + 2 * Mq) * 2.0 ** -22
+    if fmt == "kv4":
+        out, lse = L.op_attention_kv4(dtype, q, k, v, c.rows, n, 2, 1, d_h, with_lse=True)
+        assert out.isfinite().all()
+        top = scores.max(2)
+        assert (np.abs(lse[0].double().cpu().numpy() - top) <= np.abs(top) * 2.0 ** -20 + np.log(n)).all()
