@@ -10,7 +10,7 @@ A case is one pass through one operator (``op``):
 
 A 4-bit tensor is a byte buffer.  Codes [rows, Kp / 2], Kp = K rounded up to 256, zeros behind the K-th (element 2t in the low half of
 byte t; a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6).  From the next multiple of 256 bytes on one scale byte s for 32 elements, which stands
-for 2^(s - 127): [ceil(rows / 16), Kp / 256, 4, 16, 2], that of block 8 c + 4 j + b of row 16 g + r at [g, c, b, r, j].
+for 2^(s - 127): [ceil(rows / 32), Kp / 256, 2, 32, 4], that of block 8 c + 2 j + b of row 32 g + r at [g, c, b, r, j].
 """
 import math
 
@@ -144,8 +144,8 @@ def _mx4_pack(x):
     e, level, minus = _mx4_parts(torch.nn.functional.pad(x, (0, -K % 256)))
     code = (level + 8 * minus.to(torch.uint8)).flatten(1)
     codes = (code[:, 0::2] + 16 * code[:, 1::2]).flatten()
-    s = torch.nn.functional.pad((e + 127).to(torch.uint8), (0, 0, 0, -rows % 16))
-    s = s.view(s.shape[0] // 16, 16, s.shape[1] // 8, 2, 4).permute(0, 2, 4, 1, 3).flatten()   # [g, r, c, j, b] -> [g, c, b, r, j]
+    s = torch.nn.functional.pad((e + 127).to(torch.uint8), (0, 0, 0, -rows % 32))
+    s = s.view(s.shape[0] // 32, 32, s.shape[1] // 8, 4, 2).permute(0, 2, 4, 1, 3).flatten()   # [g, r, c, j, b] -> [g, c, b, r, j]
     buf = torch.zeros(_align256(codes.numel()) + s.numel(), dtype=torch.uint8, device=x.device)
     buf[:codes.numel()] = codes
     buf[_align256(codes.numel()):] = s
@@ -159,7 +159,7 @@ def _mx4_unpack(buf, rows, K):
     code = torch.stack((codes & 15, codes >> 4), -1).view(rows, Kp // 32, 32)
     v = _mx4_magnitude(code & 7)
     v = torch.where(code >= 8, -v, v)
-    s = buf[_align256(rows * Kp // 2):].view(-1, Kp // 256, 4, 16, 2).permute(0, 3, 1, 4, 2).reshape(-1, Kp // 32)[:rows]
+    s = buf[_align256(rows * Kp // 2):].view(-1, Kp // 256, 2, 32, 4).permute(0, 3, 1, 4, 2).reshape(-1, Kp // 32)[:rows]
     return torch.ldexp(v, s[..., None].to(torch.int32) - 127).view(rows, Kp)[:, :K]
 
 
@@ -297,7 +297,7 @@ def exact(case, seed):
         w[:, 1::2] = table[(raw // 16).long()]
         block = torch.arange(half // 16, device="cuda")
         row = torch.arange(N, device="cuda")[:, None]
-        at = (((row // 16 * (half // 128) + block // 8) * 4 + block % 4) * 16 + row % 16) * 2 + block % 8 // 4
+        at = (((row // 32 * (half // 128) + block // 8) * 2 + block % 2) * 32 + row % 32) * 4 + block % 8 // 2
         s = st["w"][-(-N * half // 256) * 256:][at].double()
         w *= torch.pow(2.0, s - 127).repeat_interleave(32, 1)
         return _exact_blocks(st["x"].double()) @ w[:, :K].t()
