@@ -481,6 +481,58 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
                        const float* w_scale, int32_t N, int32_t K, void* out, void* scratch, size_t scratch_bytes,
                        void* hip_stream);
 
+/* ---- from the residual stream to token log probabilities, in few bits -----------------------
+ * A sublayer's output added to the stream and its norm as rows for the maps in few bits; linear maps on 4-bit blocks, whose weights
+ * are half the bytes of 8-bit ones; and what the logits say about tokens beyond the greedy one.  Memory, scratch, captures and
+ * alignment as above, where nothing else is said; M < 2^24.
+ *
+ * s = stream[r] + x[i] (stream[r] if x is NULL), rounded to stream_dtype, r = row_idx[i] (i if NULL);
+ * h = (s * rstd) * gain in float32, rstd = 1 / sqrt(mean of s^2 + eps) rounded to float32 from 64 bits.  Row i of the result: h
+ * as dllmc_op_quant8 (norm_quant8) or dllmc_op_quant_mx4 (norm_mx4) would hold it.  x [M, d] and gain [d] of dtype, stream
+ * [stream_rows, d] of stream_dtype (dtype, or DLLMC_F32), all aligned to their elements; d <= 131072, 0 <= eps < infinity.  sum_out
+ * [M, d] of stream_dtype (may be NULL): s; it may be the stream (row_idx NULL) or, of the same type, x.  An r outside
+ * [0, stream_rows): row i becomes zeros (norm_quant8: with scale 0) and row i of sum_out is left as it was.  A row with an infinity or
+ * NaN, and one of zeros with eps = 0, becomes NaN (norm_quant8: zeros with scale NaN). */
+int dllmc_op_norm_quant8(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows,
+                         const int32_t* row_idx, int32_t M, int32_t d, const void* gain, float eps, void* sum_out, int8_t* q,
+                         float* scale, void* hip_stream);
+int dllmc_op_norm_mx4(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows, const int32_t* row_idx,
+                      int32_t M, int32_t d, const void* gain, float eps, void* sum_out, void* out, void* hip_stream);
+/* out [M, K] (aligned to its elements) row i = the values q * scale of 8-bit row r = row_idx[i] (i if NULL) of q_rows; zeros where r is no row. */
+int dllmc_op_load8(int32_t dtype, const int8_t* q, const float* scale, int32_t q_rows, int32_t K, const int32_t* row_idx, int32_t M,
+                   void* out, void* hip_stream);
+
+/* Matrix of `rows` (at most 2^24) rows of K (at most 131072) elements in 4-bit blocks: dllmc_mx4_bytes() bytes (0: invalid).  Blocks of 32
+ * neighbouring elements of a row with codes and scales as in a 4-bit cache tensor.  Codes [rows][Kp / 2], Kp = K rounded
+ * up to 256, element 2t in the low half of byte t, zeros behind the K-th; at the next multiple of 256 bytes scale bytes
+ * [ceil(rows / 32)][Kp / 256][2][32][4], that of block 8 c + 2 j + b of row 32 g + r at [g][c][b][r][j] (those of rows that are not there
+ * are never looked at). */
+size_t dllmc_mx4_bytes(int32_t rows, int32_t K);
+/* Row i of the M rows of `out` <- row r = row_idx[i] (i if NULL) of x [x_rows, K], aligned to its elements; zeros where r is no row. */
+int dllmc_op_quant_mx4(int32_t dtype, const void* x, int32_t x_rows, const int32_t* row_idx, int32_t M, int32_t K, void* out,
+                       void* hip_stream);
+/* out [M, K] (aligned to its elements) row i = the values of row r = row_idx[i] (i if NULL), exact in either dtype; zeros where r is no row. */
+int dllmc_op_mx4_load(int32_t dtype, const void* in, int32_t rows, int32_t K, const int32_t* row_idx, int32_t M, void* out,
+                      void* hip_stream);
+/* out[i][j] = sum over k of a[i][k] * w[j][k], [M, N] of dtype; a of M <= 2^22 rows, w of N, both as dllmc_op_quant_mx4 leaves them,
+ * M * N <= 2^35.  Sums are float32: products below 2^-149 add nothing, sums past its range are infinite or NaN.  scratch: at least
+ * dllmc_op_linear_mx4_scratch_bytes() bytes, which may be 0.  Bit-reproducible. */
+size_t dllmc_op_linear_mx4_scratch_bytes(int32_t M, int32_t N, int32_t K);
+int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, int32_t N, int32_t K, void* out, void* scratch,
+                        size_t scratch_bytes, void* hip_stream);
+
+/* Of every row of logits [M, vocab] (dtype; row i at i * ld elements, ld >= vocab; vocab <= 2^24): the log probabilities under its softmax
+ * of n_given <= 65536 given tokens (logp [M, n_given] for tokens [M, n_given]; minus infinity for an id outside [0, vocab)), its entropy [M],
+ * and the top_k <= 64 likeliest tokens, most likely first, of equal logits the lower id first (top_ids, top_logp [M, top_k]).  tokens and
+ * logp are NULL and n_given 0, top_ids and top_logp NULL and top_k 0, entropy NULL, where that is not asked for.  A logit of minus infinity
+ * is a token that cannot be: it adds nothing and is no alternative; where there are no more alternatives ids are -1 and log probabilities
+ * minus infinity.  A row of nothing else has log probabilities of minus infinity, entropy 0 and no alternatives; a row with a
+ * NaN or plus infinity has NaN everywhere and ids of -1.  scratch: at least dllmc_op_logprobs_scratch_bytes() bytes, which may be 0. */
+size_t dllmc_op_logprobs_scratch_bytes(int32_t dtype, int32_t M, int32_t vocab, int32_t top_k);
+int dllmc_op_logprobs(int32_t dtype, const void* logits, int32_t ld, int32_t M, int32_t vocab, const int32_t* tokens, int32_t n_given,
+                      int32_t top_k, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* scratch, size_t scratch_bytes,
+                      void* hip_stream);
+
 /* ---- achievable-peak probes (measurement aids, not steps of the method) ----
  * What this GPU delivers for the plainest kernels of each kind, so that a roofline fraction
  * can be quoted against a measured ceiling beside the published one.  All three only enqueue

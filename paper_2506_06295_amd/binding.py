@@ -38,6 +38,8 @@ EXPORTS = (
     "dllmc_op_attention_kv4", "dllmc_op_attention_weights_scratch_bytes", "dllmc_op_attention_weights", "dllmc_op_evict",
     "dllmc_op_compact", "dllmc_i8_row_bytes", "dllmc_op_quant8", "dllmc_op_linear_i8_scratch_bytes", "dllmc_op_linear_i8",
     "dllmc_plan_linear_i8", "dllmc_plan_attention_kv4", "dllmc_plan_attention_weights",
+    "dllmc_op_norm_quant8", "dllmc_op_norm_mx4", "dllmc_op_load8", "dllmc_mx4_bytes", "dllmc_op_quant_mx4", "dllmc_op_mx4_load",
+    "dllmc_op_linear_mx4_scratch_bytes", "dllmc_op_linear_mx4", "dllmc_op_logprobs_scratch_bytes", "dllmc_op_logprobs",
 )
 NUM_KERNEL_CLASSES = 13
 
@@ -214,7 +216,17 @@ def lib() -> C.CDLL:
                 ("dllmc_plan_attention_kv4", i32, [i32] * 7 + [C.POINTER(i32)] * 3),
                 ("dllmc_plan_attention_weights", i32, [i32] * 8 + [C.POINTER(i32)] * 3),
                 ("dllmc_plan_linear_i8", i32, [i32] * 3 + [C.POINTER(i32)] * 3),
-                ("dllmc_op_linear_i8", C.c_int, [i32, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, size, ptr])):
+                ("dllmc_op_linear_i8", C.c_int, [i32, ptr, ptr, i32, ptr, ptr, i32, i32, ptr, ptr, size, ptr]),
+                ("dllmc_op_norm_quant8", C.c_int, [i32, i32, ptr, ptr, i32, ptr, i32, i32, ptr, C.c_float, ptr, ptr, ptr, ptr]),
+                ("dllmc_op_norm_mx4", C.c_int, [i32, i32, ptr, ptr, i32, ptr, i32, i32, ptr, C.c_float, ptr, ptr, ptr]),
+                ("dllmc_op_load8", C.c_int, [i32, ptr, ptr, i32, i32, ptr, i32, ptr, ptr]),
+                ("dllmc_mx4_bytes", size, [i32] * 2),
+                ("dllmc_op_quant_mx4", C.c_int, [i32, ptr, i32, ptr, i32, i32, ptr, ptr]),
+                ("dllmc_op_mx4_load", C.c_int, [i32, ptr, i32, i32, ptr, i32, ptr, ptr]),
+                ("dllmc_op_linear_mx4_scratch_bytes", size, [i32] * 3),
+                ("dllmc_op_linear_mx4", C.c_int, [i32, ptr, i32, ptr, i32, i32, ptr, ptr, size, ptr]),
+                ("dllmc_op_logprobs_scratch_bytes", size, [i32] * 4),
+                ("dllmc_op_logprobs", C.c_int, [i32, ptr, i32, i32, i32, ptr, i32, i32, ptr, ptr, ptr, ptr, ptr, size, ptr])):
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
         _lib = L
@@ -792,6 +804,128 @@ def op_linear_i8(dtype: str, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Te
     _check(lib().dllmc_op_linear_i8(code, ap, sa, M, wp, sw, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream(dev)),
            "dllmc_op_linear_i8")
     return out
+
+
+# ---- from the residual stream to token log probabilities, in few bits ------------------------------
+def _norm_operands(dtype, stream, gain, x, row_idx, stream_dtype, sum_out):
+    """What the two norms take: the call's first arguments, M, d, the device and where the sum goes."""
+    code, tdt = _DTYPES[dtype]
+    scode, sdt = _DTYPES[dtype if stream_dtype is None else stream_dtype]
+    rows, d = stream.shape
+    M = rows if row_idx is None else row_idx.numel()
+    dev = _device("stream", stream)
+    sp, gp = _need("stream", stream, sdt, (rows, d), dev), _need("gain", gain, tdt, (d,), dev)
+    xp, rp = _need("x", x, tdt, (M, d), dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
+    if sum_out is None and x is not None:
+        sum_out = stream.new_empty((M, d))
+    op = _need("sum_out", sum_out, sdt, (M, d), dev)
+    return (code, scode, xp, sp, rows, rp, M, d, gp), op, sum_out, dev
+
+
+def op_norm_quant8(dtype: str, stream: torch.Tensor, gain: torch.Tensor, eps: float, x: Optional[torch.Tensor] = None,
+                   row_idx: Optional[torch.Tensor] = None, stream_dtype: Optional[str] = None,
+                   sum_out: Optional[torch.Tensor] = None):
+    """(int8 [M, i8_row_bytes(d)], float32 [M], sums [M, d]): the RMS norm of rows row_idx (int32 [M]; all if None) of stream [*, d]
+    plus x [M, d] as op_quant8 holds rows, and those sums in the stream's type (None without x and sum_out).  stream_dtype: dtype if
+    None.  sum_out: where the sums go (may be stream, or x)."""
+    args, op, sum_out, dev = _norm_operands(dtype, stream, gain, x, row_idx, stream_dtype, sum_out)
+    M, d = args[6], args[7]
+    q, scale = stream.new_empty((M, i8_row_bytes(d)), dtype=torch.int8), stream.new_empty(M, dtype=torch.float32)
+    _check(lib().dllmc_op_norm_quant8(*args, eps, op, q.data_ptr(), scale.data_ptr(), _stream(dev)), "dllmc_op_norm_quant8")
+    return q, scale, sum_out
+
+
+def op_norm_mx4(dtype: str, stream: torch.Tensor, gain: torch.Tensor, eps: float, x: Optional[torch.Tensor] = None,
+                row_idx: Optional[torch.Tensor] = None, stream_dtype: Optional[str] = None, sum_out: Optional[torch.Tensor] = None):
+    """(uint8 buffer of M rows in 4-bit blocks, sums [M, d]): as op_norm_quant8, the norm as op_quant_mx4 holds rows."""
+    args, op, sum_out, dev = _norm_operands(dtype, stream, gain, x, row_idx, stream_dtype, sum_out)
+    out = stream.new_empty(mx4_bytes(args[6], args[7]), dtype=torch.uint8)
+    _check(lib().dllmc_op_norm_mx4(*args, eps, op, out.data_ptr(), _stream(dev)), "dllmc_op_norm_mx4")
+    return out, sum_out
+
+
+def op_load8(dtype: str, q: torch.Tensor, scale: torch.Tensor, K: int, row_idx: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """[M, K]: the values of rows row_idx (int32 [M]; all if None) of 8-bit rows as op_quant8 gives them."""
+    code, tdt = _DTYPES[dtype]
+    rows = q.shape[0]
+    M = rows if row_idx is None else row_idx.numel()
+    dev = _device("q", q)
+    qp, sp = _need("q", q, torch.int8, (rows, i8_row_bytes(K)), dev), _need("scale", scale, torch.float32, (rows,), dev)
+    rp = _need("row_idx", row_idx, torch.int32, (M,), dev)
+    out = q.new_empty((M, K), dtype=tdt)
+    _check(lib().dllmc_op_load8(code, qp, sp, rows, K, rp, M, out.data_ptr(), _stream(dev)), "dllmc_op_load8")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def mx4_bytes(rows: int, K: int) -> int:
+    """Bytes of a matrix of rows x K in 4-bit blocks (a uint8 tensor of that size holds it)."""
+    n = lib().dllmc_mx4_bytes(rows, K) if all(0 < v < 1 << 31 for v in (rows, K)) else 0  # (of 32 bits)
+    if n == 0:
+        raise DllmcError(f"dllmc_mx4_bytes: no 4-bit blocks of {rows} rows of {K}")
+    return n
+
+
+def op_quant_mx4(dtype: str, x: torch.Tensor, row_idx: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """uint8 buffer: rows of x [*, K] (those that row_idx int32 [M] names, zeros where it names none) in 4-bit blocks."""
+    code, tdt = _DTYPES[dtype]
+    rows, K = x.shape
+    M = rows if row_idx is None else row_idx.numel()
+    dev = _device("x", x)
+    xp, rp = _need("x", x, tdt, (rows, K), dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
+    out = x.new_empty(mx4_bytes(M, K), dtype=torch.uint8)
+    _check(lib().dllmc_op_quant_mx4(code, xp, rows, rp, M, K, out.data_ptr(), _stream(dev)), "dllmc_op_quant_mx4")
+    return out
+
+
+def op_mx4_load(dtype: str, mx: torch.Tensor, rows: int, K: int, row_idx: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """[M, K]: the values of rows row_idx (int32 [M]; all if None) of a matrix of rows x K in 4-bit blocks."""
+    code, tdt = _DTYPES[dtype]
+    M = rows if row_idx is None else row_idx.numel()
+    dev = _device("mx", mx)
+    mp, rp = _need("mx", mx, torch.uint8, (mx4_bytes(rows, K),), dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
+    out = mx.new_empty((M, K), dtype=tdt)
+    _check(lib().dllmc_op_mx4_load(code, mp, rows, K, rp, M, out.data_ptr(), _stream(dev)), "dllmc_op_mx4_load")
+    return out
+
+
+def op_linear_mx4(dtype: str, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int) -> torch.Tensor:
+    """[M, N] of dtype: M rows a times N rows w, K elements each, both in 4-bit blocks as op_quant_mx4 gives them."""
+    code, tdt = _DTYPES[dtype]
+    dev = _device("a", a)
+    ap, wp = _need("a", a, torch.uint8, (mx4_bytes(M, K),), dev), _need("w", w, torch.uint8, (mx4_bytes(N, K),), dev)
+    out = a.new_empty((M, N), dtype=tdt)
+    nbytes = _scratch_bytes("linear_mx4", M, N, K)
+    scratch = _scratch(nbytes, out)
+    _check(lib().dllmc_op_linear_mx4(code, ap, M, wp, N, K, out.data_ptr(), _ptr(scratch), nbytes, _stream(dev)), "dllmc_op_linear_mx4")
+    return out
+
+
+def op_logprobs(dtype: str, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0):
+    """(logp [M, n], entropy [M], top_ids int32 [M, top_k], top_logp [M, top_k]) of logits [M, vocab], float32 unless said: log
+    probabilities of tokens (int32 [M, n]; None without), the entropy, and the likeliest tokens (None without top_k).  The rows of logits
+    may lie apart (a slice of wider ones)."""
+    code, tdt = _DTYPES[dtype]
+    M, vocab = logits.shape
+    dev = _device("logits", logits)
+    ld = logits.stride(0) if M > 1 else vocab
+    if logits.dtype is not tdt or (vocab > 1 and logits.stride(1) != 1) or not vocab <= ld < 1 << 31:
+        raise DllmcError(f"logits: need a {tdt} tensor of whole rows, got {logits.dtype} {tuple(logits.shape)} of strides {logits.stride()}")
+    if not 0 <= top_k < 1 << 31 or M >= 1 << 31:
+        raise DllmcError(f"op_logprobs: no {top_k} tokens of {M} rows")  # (what is allocated goes by them, and the call takes 32 bits)
+    n = 0 if tokens is None else tokens.shape[-1]
+    tp = _need("tokens", tokens, torch.int32, (M, n), dev)
+    entropy = logits.new_empty(M, dtype=torch.float32)
+    logp = None if tokens is None else logits.new_empty((M, n), dtype=torch.float32)
+    ids = top = None
+    if top_k:
+        top = logits.new_empty((M, top_k), dtype=torch.float32)
+        ids = torch.empty_like(top, dtype=torch.int32)
+    nbytes = _scratch_bytes("logprobs", code, M, vocab, top_k)
+    scratch = _scratch(nbytes, logits)
+    _check(lib().dllmc_op_logprobs(code, logits.data_ptr(), ld, M, vocab, tp, n, top_k, _ptr(logp), entropy.data_ptr(), _ptr(ids),
+                                   _ptr(top), _ptr(scratch), nbytes, _stream(dev)), "dllmc_op_logprobs")
+    return logp, entropy, ids, top
 
 
 def probe_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

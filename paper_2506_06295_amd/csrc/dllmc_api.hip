@@ -10,6 +10,7 @@
 #include "../../include/dllmc.h"
 #include "common.hpp"
 #include "kv4.hpp"
+#include "mx4.hpp"
 #include "paging_host.hpp"
 
 using namespace dllmc;
@@ -1426,6 +1427,174 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
     if (need && !apart(scratch, need, i.p, i.n)) return DLLMC_EINVAL;
   (void)hipGetLastError();
   launch_linear_i8(plan, dtype, a, a_scale, M, w, w_scale, N, K, out, scratch, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+}  // extern "C"
+
+// ---- from the residual stream to token log probabilities in few bits --------------------------------
+
+namespace {
+struct Bytes { const void* p; size_t n; };
+template <int A> bool clear_of(const void* p, size_t n, const Bytes (&from)[A]) {
+  for (const Bytes& f : from)
+    if (f.p && !apart(p, n, f.p, f.n)) return false;
+  return true;
+}
+inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+bool mx4_shape_ok(int32_t rows, int32_t K) { return rows >= 1 && rows <= kMaxRows && K >= 1 && K <= kMaxI8K; }
+// (results are counted in workgroups of a launch, and a launch has fewer than 2^32 work-items)
+bool linear_mx4_ok(int32_t M, int32_t N, int32_t K) {
+  return M <= kMaxI8M && mx4_shape_ok(M, K) && mx4_shape_ok(N, K) && static_cast<long long>(M) * N <= (1ll << 35);
+}
+
+// operands of the two norms; out, out2: the results besides the sum
+bool norm_ok(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows, const int32_t* row_idx,
+             int32_t M, int32_t d, const void* gain, float eps, const void* sum_out, const Bytes& out, const Bytes& out2) {
+  if (!dtype_ok(dtype) || !dtype_ok(stream_dtype) || (dtype == DLLMC_F32 && stream_dtype != DLLMC_F32)) return false;
+  if (!stream || !gain || !out.p || M < 1 || M >= kMaxRows || d < 1 || d > kMaxI8K || stream_rows < 1) return false;
+  if (row_idx == nullptr && M > stream_rows) return false;
+  if (!(eps >= 0.f) || !(eps < INFINITY)) return false;
+  const size_t esz = elem_bytes(dtype), ssz = elem_bytes(stream_dtype);
+  if (!aligned_to(x, esz) || !aligned_to(gain, esz) || !aligned_to(stream, ssz) || !aligned_to(sum_out, ssz) || !aligned4(row_idx))
+    return false;
+  const size_t md = static_cast<size_t>(M) * d;
+  const Bytes in[] = {{x, md * esz}, {gain, d * esz}, {stream, static_cast<size_t>(stream_rows) * d * ssz},
+                      {row_idx, static_cast<size_t>(M) * 4}};
+  if (!clear_of(out.p, out.n, in) || (out2.p && !clear_of(out2.p, out2.n, in))) return false;
+  if (out2.p && !apart(out.p, out.n, out2.p, out2.n)) return false;
+  if (!sum_out) return true;
+  // the sum may take the place of what it is the sum of, row for row
+  const bool in_stream = sum_out == stream && row_idx == nullptr, in_x = sum_out == x && dtype == stream_dtype;
+  const Bytes rest[] = {{in_x ? nullptr : x, md * esz}, {gain, d * esz}, {in_stream ? nullptr : stream, in[2].n}, in[3], out, out2};
+  return clear_of(sum_out, md * ssz, rest);
+}
+}  // namespace
+
+extern "C" {
+
+int dllmc_op_norm_quant8(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows,
+                         const int32_t* row_idx, int32_t M, int32_t d, const void* gain, float eps, void* sum_out, int8_t* q,
+                         float* scale, void* hip_stream) {
+  if (M < 1 || d < 1 || d > kMaxI8K || !q || !scale || !aligned16(q) || !aligned4(scale)) return DLLMC_EINVAL;
+  if (!norm_ok(dtype, stream_dtype, x, stream, stream_rows, row_idx, M, d, gain, eps, sum_out, Bytes{q, M * i8_row_bytes(d)},
+               Bytes{scale, static_cast<size_t>(M) * 4}))
+    return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_norm_quant8(dtype, stream_dtype, NormRows{x, stream, row_idx, gain, sum_out, stream_rows, M, d, eps}, q, scale,
+                     static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_norm_mx4(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows, const int32_t* row_idx,
+                      int32_t M, int32_t d, const void* gain, float eps, void* sum_out, void* out, void* hip_stream) {
+  if (!mx4_shape_ok(M, d) || !out || !aligned16(out)) return DLLMC_EINVAL;
+  if (!norm_ok(dtype, stream_dtype, x, stream, stream_rows, row_idx, M, d, gain, eps, sum_out, Bytes{out, mx4_bytes(M, d)},
+               Bytes{nullptr, 0}))
+    return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_norm_mx4(dtype, stream_dtype, NormRows{x, stream, row_idx, gain, sum_out, stream_rows, M, d, eps}, mx4_tensor(out, M, d),
+                  static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_load8(int32_t dtype, const int8_t* q, const float* scale, int32_t q_rows, int32_t K, const int32_t* row_idx, int32_t M,
+                   void* out, void* hip_stream) {
+  if (!dtype_ok(dtype) || !q || !scale || !out || M < 1 || M >= kMaxRows || q_rows < 1 || (row_idx == nullptr && M > q_rows) || K < 1 ||
+      K > kMaxI8K || !aligned16(q) || !aligned4(scale) || !aligned4(row_idx) || !aligned_to(out, elem_bytes(dtype)))
+    return DLLMC_EINVAL;
+  const Bytes in[] = {{q, q_rows * i8_row_bytes(K)}, {scale, static_cast<size_t>(q_rows) * 4}, {row_idx, static_cast<size_t>(M) * 4}};
+  if (!clear_of(out, static_cast<size_t>(M) * K * elem_bytes(dtype), in)) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_load8(dtype, q, scale, q_rows, K, row_idx, M, out, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_mx4_bytes(int32_t rows, int32_t K) { return mx4_shape_ok(rows, K) ? mx4_bytes(rows, K) : 0; }
+
+int dllmc_op_quant_mx4(int32_t dtype, const void* x, int32_t x_rows, const int32_t* row_idx, int32_t M, int32_t K, void* out,
+                       void* hip_stream) {
+  if (!dtype_ok(dtype) || !x || !out || M >= kMaxRows || !mx4_shape_ok(M, K) || x_rows < 1 || (row_idx == nullptr && M > x_rows) ||
+      !aligned16(out) || !aligned4(row_idx) || !aligned_to(x, elem_bytes(dtype)))
+    return DLLMC_EINVAL;
+  const Bytes in[] = {{x, static_cast<size_t>(x_rows) * K * elem_bytes(dtype)}, {row_idx, static_cast<size_t>(M) * 4}};
+  if (!clear_of(out, mx4_bytes(M, K), in)) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_quant_mx4(dtype, x, x_rows, row_idx, M, K, mx4_tensor(out, M, K), static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+int dllmc_op_mx4_load(int32_t dtype, const void* in, int32_t rows, int32_t K, const int32_t* row_idx, int32_t M, void* out,
+                      void* hip_stream) {
+  if (!dtype_ok(dtype) || !in || !out || !mx4_shape_ok(rows, K) || M < 1 || M >= kMaxRows || (row_idx == nullptr && M > rows) ||
+      !aligned16(in) || !aligned4(row_idx) || !aligned_to(out, elem_bytes(dtype)))
+    return DLLMC_EINVAL;
+  const Bytes from[] = {{in, mx4_bytes(rows, K)}, {row_idx, static_cast<size_t>(M) * 4}};
+  if (!clear_of(out, static_cast<size_t>(M) * K * elem_bytes(dtype), from)) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_mx4_load(dtype, mx4_tensor(in, rows, K), row_idx, M, K, out, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_op_linear_mx4_scratch_bytes(int32_t M, int32_t N, int32_t K) {
+  return linear_mx4_ok(M, N, K) ? linear_mx4_scratch_bytes(M, N, mx4_width(K)) : 0;
+}
+
+int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, int32_t N, int32_t K, void* out, void* scratch,
+                        size_t scratch_bytes, void* hip_stream) {
+  if (!dtype_ok(dtype) || !a || !w || !out || !linear_mx4_ok(M, N, K) || !aligned16(a) || !aligned16(w) || !aligned16(out) ||
+      !aligned16(scratch))
+    return DLLMC_EINVAL;
+  const size_t need = linear_mx4_scratch_bytes(M, N, mx4_width(K)), ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
+  const Bytes in[] = {{a, mx4_bytes(M, K)}, {w, mx4_bytes(N, K)}};
+  if (!clear_of(out, ob, in)) return DLLMC_EINVAL;
+  if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  if (need && (!apart(scratch, need, out, ob) || !clear_of(scratch, need, in))) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_linear_mx4(dtype, mx4_tensor(a, M, K), mx4_tensor(w, N, K), out, scratch, static_cast<hipStream_t>(hip_stream));
+  HIP_TRY(hipGetLastError());
+  return DLLMC_OK;
+}
+
+size_t dllmc_op_logprobs_scratch_bytes(int32_t dtype, int32_t M, int32_t vocab, int32_t top_k) {
+  if (!dtype_ok(dtype) || M < 1 || M >= kMaxRows || vocab < 1 || vocab > kMaxRows || top_k < 0 || top_k > kMaxTop) return 0;
+  return logprobs_scratch_bytes(dtype, M, vocab, top_k);
+}
+
+int dllmc_op_logprobs(int32_t dtype, const void* logits, int32_t ld, int32_t M, int32_t vocab, const int32_t* tokens, int32_t n_given,
+                      int32_t top_k, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* scratch, size_t scratch_bytes,
+                      void* hip_stream) {
+  if (!dtype_ok(dtype) || !logits || M < 1 || M >= kMaxRows || vocab < 1 || vocab > kMaxRows || ld < vocab || n_given < 0 ||
+      n_given > kMaxWidth || top_k < 0 || top_k > kMaxTop)
+    return DLLMC_EINVAL;
+  if ((n_given > 0) != (tokens != nullptr) || (n_given > 0) != (logp != nullptr) || (top_k > 0) != (top_ids != nullptr) ||
+      (top_k > 0) != (top_logp != nullptr) || (!logp && !entropy && !top_ids))
+    return DLLMC_EINVAL;
+  if (!aligned_to(logits, elem_bytes(dtype)) || !aligned4(tokens) || !aligned4(logp) || !aligned4(entropy) || !aligned4(top_ids) ||
+      !aligned4(top_logp) || !aligned16(scratch))
+    return DLLMC_EINVAL;
+  const size_t m = static_cast<size_t>(M), given = m * n_given * 4, top = m * top_k * 4;
+  const Bytes in[] = {{logits, ((m - 1) * ld + vocab) * elem_bytes(dtype)}, {tokens, given}};
+  const Bytes res[] = {{logp, given}, {entropy, m * 4}, {top_ids, top}, {top_logp, top}};
+  const size_t need = logprobs_scratch_bytes(dtype, M, vocab, top_k);
+  for (int i = 0; i < 4; ++i) {
+    if (!res[i].p) continue;
+    if (!clear_of(res[i].p, res[i].n, in)) return DLLMC_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (res[j].p && !apart(res[i].p, res[i].n, res[j].p, res[j].n)) return DLLMC_EINVAL;
+  }
+  if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
+  if (need && (!clear_of(scratch, need, in) || !clear_of(scratch, need, res))) return DLLMC_EINVAL;
+  (void)hipGetLastError();
+  launch_logprobs(dtype, LogprobRows{logits, ld, M, vocab, tokens, n_given, top_k, logp, entropy, top_ids, top_logp}, scratch,
+                  static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
   return DLLMC_OK;
 }

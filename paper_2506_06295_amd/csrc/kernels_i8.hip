@@ -18,29 +18,6 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // ---- quantising rows --------------------------------------------------------------------------------------
-// Rows below this largest magnitude count as zeros: 127 times its reciprocal stays finite.
-constexpr float kTiny = 1.17549435e-38f * 256.f;
-
-struct RowScale {
-  float f, scale;  // q = rint(x * f)
-  bool finite;
-};
-__device__ __forceinline__ RowScale row_scale(uint32_t top) {
-  const float m = __uint_as_float(top);
-  const bool finite = top < 0x7f800000u, some = finite && m >= kTiny;
-  return {some ? 127.f * (1.f / m) : 0.f, !finite ? __uint_as_float(0x7fc00000u) : some ? m / 127.f : 0.f, finite};
-}
-template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o, 64)));
-  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) v = max(v, red[w]);
-  return v;
-}
-
 // q = rint(x * (127 * (1 / max|x|))) in float32 (what 127 / tensor is where a tensor's reciprocal is multiplied: the same codes as a
 // plain program's), scale = max|x| / 127; one workgroup per row, the row in registers (PC pieces of eight elements a
 // thread).  Bound by the bytes with many rows, by two trips to memory with few.

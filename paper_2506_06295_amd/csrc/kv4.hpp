@@ -114,6 +114,30 @@ template <> struct Eight<bf16_t> {
   }
 };
 
+// ---- 8-bit rows
+// Rows below this largest magnitude count as zeros: 127 times its reciprocal stays finite.
+constexpr float kTiny = 1.17549435e-38f * 256.f;
+
+struct RowScale {
+  float f, scale;  // q = rint(x * f)
+  bool finite;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t top) {
+  const float m = __uint_as_float(top);
+  const bool finite = top < 0x7f800000u, some = finite && m >= kTiny;
+  return {some ? 127.f * (1.f / m) : 0.f, !finite ? __uint_as_float(0x7fc00000u) : some ? m / 127.f : 0.f, finite};
+}
+template <int NW> __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o, 64)));
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) v = max(v, red[w]);
+  return v;
+}
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <typename T> struct Parts;  // bf16 parts of a query element and of a probability
