@@ -340,6 +340,9 @@ int32_t dllmc_plan_attention_weights(int32_t dtype, int32_t cache_format, int32_
  * wavefronts share it. */
 int32_t dllmc_plan_linear_i8(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole);
 
+/* Host-only: the same of dllmc_op_linear_mx4. */
+int32_t dllmc_plan_linear_mx4(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole);
+
 /* Host-only: the number of key ranges of a bf16 attention of Mq < 128 queries per sequence with head width 128
  * (split_keys: with a scratch buffer).  *queries (may be NULL): queries per workgroup of the kernel whose
  * wavefronts split the keys, 16, 32 or 64; 0: 64 queries whose wavefronts walk all keys together; -1: the
@@ -521,7 +524,7 @@ size_t dllmc_op_linear_mx4_scratch_bytes(int32_t M, int32_t N, int32_t K);
 int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, int32_t N, int32_t K, void* out, void* scratch,
                         size_t scratch_bytes, void* hip_stream);
 
-/* Of every row of logits [M, vocab] (dtype; row i at i * ld elements, ld >= vocab; vocab <= 2^24): the log probabilities under its softmax
+/* Of every row of logits [M, vocab] (dtype; row i at i * ld elements, ld >= vocab; M < 2^23, vocab <= 2^24, M * vocab <= 2^40): the log probabilities under its softmax
  * of n_given <= 65536 given tokens (logp [M, n_given] for tokens [M, n_given]; minus infinity for an id outside [0, vocab)), its entropy [M],
  * and the top_k <= 64 likeliest tokens, most likely first, of equal logits the lower id first (top_ids, top_logp [M, top_k]).  tokens and
  * logp are NULL and n_given 0, top_ids and top_logp NULL and top_k 0, entropy NULL, where that is not asked for.  A logit of minus infinity

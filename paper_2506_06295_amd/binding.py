@@ -39,6 +39,7 @@ EXPORTS = (
     "dllmc_op_compact", "dllmc_i8_row_bytes", "dllmc_op_quant8", "dllmc_op_linear_i8_scratch_bytes", "dllmc_op_linear_i8",
     "dllmc_plan_linear_i8", "dllmc_plan_attention_kv4", "dllmc_plan_attention_weights",
     "dllmc_op_norm_quant8", "dllmc_op_norm_mx4", "dllmc_op_load8", "dllmc_mx4_bytes", "dllmc_op_quant_mx4", "dllmc_op_mx4_load",
+    "dllmc_plan_linear_mx4",
     "dllmc_op_linear_mx4_scratch_bytes", "dllmc_op_linear_mx4", "dllmc_op_logprobs_scratch_bytes", "dllmc_op_logprobs",
 )
 NUM_KERNEL_CLASSES = 13
@@ -223,6 +224,7 @@ def lib() -> C.CDLL:
                 ("dllmc_mx4_bytes", size, [i32] * 2),
                 ("dllmc_op_quant_mx4", C.c_int, [i32, ptr, i32, ptr, i32, i32, ptr, ptr]),
                 ("dllmc_op_mx4_load", C.c_int, [i32, ptr, i32, i32, ptr, i32, ptr, ptr]),
+                ("dllmc_plan_linear_mx4", i32, [i32] * 3 + [C.POINTER(i32)] * 3),
                 ("dllmc_op_linear_mx4_scratch_bytes", size, [i32] * 3),
                 ("dllmc_op_linear_mx4", C.c_int, [i32, ptr, i32, ptr, i32, i32, ptr, ptr, size, ptr]),
                 ("dllmc_op_logprobs_scratch_bytes", size, [i32] * 4),
@@ -887,6 +889,15 @@ def op_mx4_load(dtype: str, mx: torch.Tensor, rows: int, K: int, row_idx: Option
     out = mx.new_empty((M, K), dtype=tdt)
     _check(lib().dllmc_op_mx4_load(code, mp, rows, K, rp, M, out.data_ptr(), _stream(dev)), "dllmc_op_mx4_load")
     return out
+
+
+def plan_linear_mx4(M: int, N: int, K: int):
+    """(rows, columns) of op_linear_mx4's tiles, slices of the contraction, whether it takes the tile kernels; no GPU needed."""
+    cols, slices, whole = C.c_int32(), C.c_int32(), C.c_int32()
+    rows = lib().dllmc_plan_linear_mx4(M, N, K, C.byref(cols), C.byref(slices), C.byref(whole))
+    if rows < 1:
+        raise DllmcError("dllmc_plan_linear_mx4: invalid argument")
+    return (rows, cols.value), slices.value, bool(whole.value)
 
 
 def op_linear_mx4(dtype: str, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int) -> torch.Tensor:

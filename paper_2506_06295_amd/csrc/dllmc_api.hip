@@ -1450,6 +1450,11 @@ bool linear_mx4_ok(int32_t M, int32_t N, int32_t K) {
   return M <= kMaxI8M && mx4_shape_ok(M, K) && mx4_shape_ok(N, K) && static_cast<long long>(M) * N <= (1ll << 35);
 }
 
+// (workgroups: at most one for every row and one for 2^18 logits, fewer than 2^24)
+bool logits_ok(int32_t M, int32_t vocab) {
+  return M >= 1 && M < kMaxRows / 2 && vocab >= 1 && vocab <= kMaxRows && static_cast<long long>(M) * vocab <= (1ll << 40);
+}
+
 // operands of the two norms; out, out2: the results besides the sum
 bool norm_ok(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows, const int32_t* row_idx,
              int32_t M, int32_t d, const void* gain, float eps, const void* sum_out, const Bytes& out, const Bytes& out2) {
@@ -1543,8 +1548,17 @@ int dllmc_op_mx4_load(int32_t dtype, const void* in, int32_t rows, int32_t K, co
   return DLLMC_OK;
 }
 
+int32_t dllmc_plan_linear_mx4(int32_t M, int32_t N, int32_t K, int32_t* cols, int32_t* slices, int32_t* whole) {
+  if (!linear_mx4_ok(M, N, K)) return DLLMC_EINVAL;
+  const Mx4Plan p = plan_mx4(M, N, mx4_width(K));
+  if (cols) *cols = p.bn;
+  if (slices) *slices = p.S;
+  if (whole) *whole = p.wide;
+  return p.bm;
+}
+
 size_t dllmc_op_linear_mx4_scratch_bytes(int32_t M, int32_t N, int32_t K) {
-  return linear_mx4_ok(M, N, K) ? linear_mx4_scratch_bytes(M, N, mx4_width(K)) : 0;
+  return linear_mx4_ok(M, N, K) ? linear_mx4_scratch_bytes(plan_mx4(M, N, mx4_width(K)), M, N) : 0;
 }
 
 int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, int32_t N, int32_t K, void* out, void* scratch,
@@ -1552,27 +1566,27 @@ int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, 
   if (!dtype_ok(dtype) || !a || !w || !out || !linear_mx4_ok(M, N, K) || !aligned16(a) || !aligned16(w) || !aligned16(out) ||
       !aligned16(scratch))
     return DLLMC_EINVAL;
-  const size_t need = linear_mx4_scratch_bytes(M, N, mx4_width(K)), ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
+  const Mx4Plan plan = plan_mx4(M, N, mx4_width(K));
+  const size_t need = linear_mx4_scratch_bytes(plan, M, N), ob = static_cast<size_t>(M) * N * elem_bytes(dtype);
   const Bytes in[] = {{a, mx4_bytes(M, K)}, {w, mx4_bytes(N, K)}};
   if (!clear_of(out, ob, in)) return DLLMC_EINVAL;
   if (need && (!scratch || scratch_bytes < need)) return DLLMC_ENOMEM;
   if (need && (!apart(scratch, need, out, ob) || !clear_of(scratch, need, in))) return DLLMC_EINVAL;
   (void)hipGetLastError();
-  launch_linear_mx4(dtype, mx4_tensor(a, M, K), mx4_tensor(w, N, K), out, scratch, static_cast<hipStream_t>(hip_stream));
+  launch_linear_mx4(plan, dtype, mx4_tensor(a, M, K), mx4_tensor(w, N, K), out, scratch, static_cast<hipStream_t>(hip_stream));
   HIP_TRY(hipGetLastError());
   return DLLMC_OK;
 }
 
 size_t dllmc_op_logprobs_scratch_bytes(int32_t dtype, int32_t M, int32_t vocab, int32_t top_k) {
-  if (!dtype_ok(dtype) || M < 1 || M >= kMaxRows || vocab < 1 || vocab > kMaxRows || top_k < 0 || top_k > kMaxTop) return 0;
+  if (!dtype_ok(dtype) || !logits_ok(M, vocab) || top_k < 0 || top_k > kMaxTop) return 0;
   return logprobs_scratch_bytes(dtype, M, vocab, top_k);
 }
 
 int dllmc_op_logprobs(int32_t dtype, const void* logits, int32_t ld, int32_t M, int32_t vocab, const int32_t* tokens, int32_t n_given,
                       int32_t top_k, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* scratch, size_t scratch_bytes,
                       void* hip_stream) {
-  if (!dtype_ok(dtype) || !logits || M < 1 || M >= kMaxRows || vocab < 1 || vocab > kMaxRows || ld < vocab || n_given < 0 ||
-      n_given > kMaxWidth || top_k < 0 || top_k > kMaxTop)
+  if (!dtype_ok(dtype) || !logits || !logits_ok(M, vocab) || ld < vocab || n_given < 0 || n_given > kMaxWidth || top_k < 0 || top_k > kMaxTop)
     return DLLMC_EINVAL;
   if ((n_given > 0) != (tokens != nullptr) || (n_given > 0) != (logp != nullptr) || (top_k > 0) != (top_ids != nullptr) ||
       (top_k > 0) != (top_logp != nullptr) || (!logp && !entropy && !top_ids))

@@ -3,6 +3,8 @@
 // A block is 32 neighbouring elements of a row: codes of 4 bits (sign, and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) times one power of two, as
 // in a 4-bit cache.  The scaled matrix instructions multiply codes exactly and take both blocks' powers of two along, so the only roundings of
 // out[i][j] = sum_k a[i][k] w[j][k] are those of float32 sums and of the result.
+#include <type_traits>
+
 #include "mx4.hpp"
 
 namespace dllmc {
@@ -67,41 +69,400 @@ __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, con
 }
 
 // ---- the product ------------------------------------------------------------------------------------------
-// A wavefront per 32 x 32 results, operands from memory straight into registers.  The product is taken as W A^T, so that a lane holds
-// four neighbouring columns of a row; lane l has row l % 32 of either operand, elements 32 (l / 32) .. + 31 of a step of 64.
+// Products are taken as W A^T, so that a lane holds neighbouring columns of a row.  Rows past M and N repeat the last one (their scales are those
+// of the last rows' group) and are dropped at the store.
+__device__ __forceinline__ i32x8 operand(const uint4& u) {  // (a 4-bit operand is the first four registers)
+  return i32x8{static_cast<int>(u.x), static_cast<int>(u.y), static_cast<int>(u.z), static_cast<int>(u.w), 0, 0, 0, 0};
+}
+
+// four neighbouring results of a row, n0 + 4 <= N or element by element
 template <typename T>
-__global__ __launch_bounds__(256) void k_mx4_plain(Mx4Tensor a, Mx4Tensor w, T* __restrict__ out) {
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, ln = lane % 32, lg = lane / 32;
-  const int M = a.rows, N = w.rows, Kp = a.Kp;
-  const int nt = (N + 127) / 128;
-  const int m0 = blockIdx.x / nt * 32, n0 = (blockIdx.x % nt * 4 + wave) * 32;
-  if (n0 >= N) return;
-  const uint8_t* ar = a.codes + static_cast<size_t>(min(m0 + ln, M - 1)) * (Kp / 2) + lg * 16;
-  const uint8_t* wr = w.codes + static_cast<size_t>(min(n0 + ln, N - 1)) * (Kp / 2) + lg * 16;
-  const uint32_t* as = reinterpret_cast<const uint32_t*>(a.scales) + static_cast<size_t>(m0 / 32) * (Kp / 256) * 64 + lane;
-  const uint32_t* ws = reinterpret_cast<const uint32_t*>(w.scales) + static_cast<size_t>(n0 / 32) * (Kp / 256) * 64 + lane;
-  f32x16 acc = {0.f};
-  for (int c = 0; c < Kp / 256; ++c) {
-    const int sa = static_cast<int>(as[c * 64]), sw = static_cast<int>(ws[c * 64]);
-    i32x8 x[4], y[4];
+__device__ __forceinline__ void store4(T* p, int n, int N, bool whole, float a, float b, float c, float d) {
+  if (whole) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+    else *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+  } else {
+    if (n < N) stf(p, a);
+    if (n + 1 < N) stf(p + 1, b);
+    if (n + 2 < N) stf(p + 2, c);
+    if (n + 3 < N) stf(p + 3, d);
+  }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------
+// k_mx4_ring<RG, RB, NB>: tile = 16 RG RB rows x 16 NB weight rows, one workgroup of eight wavefronts per CU.  Codes and scales of both operands go
+// from global memory straight into LDS through a ring of stages.  RG wavefronts take 16 RB rows each, 8 / RG share the
+// contraction: a stage is 64 * 8 / RG bytes of every row's codes, and a wavefront multiplies its own 64 of them, 128 elements, with one 16 x 16 x 128
+// product a block.  Their sums meet in LDS at the end, in one order.  Slice blockIdx.z of the contraction; with one slice results leave
+// rounded, else as float32 sums for k_mx4_sum.
+template <int RG, int RB, int NB> struct Mx4Ring {
+  static constexpr int KW = 8 / RG, SS = KW / 2;  // wavefronts along the contraction, 128-byte lines of a stage
+  static constexpr int BM = 16 * RG * RB, R = BM + 16 * NB;
+  static constexpr int kUnits = R / 16, UL = (kUnits + 7) / 8;  // 16 rows' scales of a line (128 bytes), loads of eight of them
+  static constexpr int kCodes = R * 8 * SS, kStage = kCodes + UL * SS * 64;  // 16-byte slots
+  static constexpr int kFit = (160 * 1024) / (kStage * 16), NST = kFit > 8 ? 8 : kFit;
+  static constexpr int TC = R / 8 * SS, T = TC + UL * SS;  // load instructions of a stage, those of the codes first
+  static constexpr int L = T / 8, LR = T % 8;              // per wavefront, one more for the first LR
+};
+
+template <typename T, int RG, int RB, int NB>
+__device__ __forceinline__ void mx4_ring_body(const Mx4Tensor& a, const Mx4Tensor& w, int per_slice, T* __restrict__ out,
+                                              float* __restrict__ sums) {
+  typedef Mx4Ring<RG, RB, NB> S;
+  constexpr int NST = S::NST, SS = S::SS, R = S::R, BM = S::BM;
+  static_assert(SS >= 1 && NST >= 2, "");
+  __shared__ __attribute__((aligned(1024))) uint4 lds[NST][S::kStage];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int ln = lane % 16, lg = lane / 16;
+  const int wr = wave % RG, kk = wave / RG;
+  const int M = a.rows, N = w.rows, row_bytes = a.Kp / 2, all_lines = a.Kp / 256;
+  int col_tile, row_tile;
+  xcd_tile_map(col_tile, row_tile);
+  const int m0 = row_tile * BM, n0 = col_tile * 16 * NB;
+  const int line0 = blockIdx.z * per_slice, lines = min(all_lines, line0 + per_slice) - line0;
+  const int nkt = (lines + SS - 1) / SS;
+
+  // loader: instruction q < TC of a stage copies the codes of rows 8 (q % (R/8)) .. + 7 of line q / (R/8) (lane: row lane/8, slot lane%8, chunk
+  // slot ^ row % 8), the others the scales of eight units of a line (lane: unit lane/8, and of its [2][16] rows' four bytes the lane%8-th 16)
+  const uint8_t* src[S::L + 1];
+  int sub[S::L + 1], step[S::L + 1];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4 u = *reinterpret_cast<const uint4*>(ar + c * 128 + j * 32), v = *reinterpret_cast<const uint4*>(wr + c * 128 + j * 32);
-      x[j] = i32x8{static_cast<int>(u.x), static_cast<int>(u.y), static_cast<int>(u.z), static_cast<int>(u.w), 0, 0, 0, 0};
-      y[j] = i32x8{static_cast<int>(v.x), static_cast<int>(v.y), static_cast<int>(v.z), static_cast<int>(v.w), 0, 0, 0, 0};
+  for (int j = 0; j < S::L + 1; ++j) {
+    const int q = min(wave + 8 * j, S::T - 1);
+    if (q < S::TC) {
+      const int r = q % (R / 8) * 8 + lane / 8;
+      const uint8_t* row = r < BM ? a.codes + static_cast<size_t>(min(m0 + r, M - 1)) * row_bytes
+                                  : w.codes + static_cast<size_t>(min(n0 + r - BM, N - 1)) * row_bytes;
+      src[j] = row + static_cast<size_t>(line0) * 128 + ((lane % 8) ^ (lane / 8)) * 16;
+      sub[j] = q / (R / 8);
+      step[j] = 128;
+    } else {
+      const int u = min((q - S::TC) % S::UL * 8 + lane / 8, S::kUnits - 1);
+      const Mx4Tensor& t = u < BM / 16 ? a : w;
+      const int r = min(u < BM / 16 ? m0 + u * 16 : n0 + u * 16 - BM, (t.rows - 1) / 16 * 16);  // (a unit's first row)
+      src[j] = t.scales + (static_cast<size_t>(r / 32) * all_lines + line0) * 256 + lane % 8 / 4 * 128 + r % 32 * 4 + lane % 4 * 16;
+      sub[j] = (q - S::TC) / S::UL;
+      step[j] = 256;
     }
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[0], x[0], acc, 4, 4, 0, sw, 0, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[1], x[1], acc, 4, 4, 1, sw, 1, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[2], x[2], acc, 4, 4, 2, sw, 2, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[3], x[3], acc, 4, 4, 3, sw, 3, sa);
   }
-  const int m = m0 + ln;
-  if (m >= M) return;
+  // the walk starts at a stage that depends on the column tile: unrotated every load in flight has the same address bits
+  // below the row pitch
+  const int rot = (col_tile % 8 * 8 + col_tile / 8) % nkt;
+  auto issue_one = [&](int stage, int kt, int j) {
+    const int q = wave + 8 * j;
+    const int line = min(kt * SS + sub[j], lines - 1);  // (lines past the last one repeat it and are not multiplied)
+    __builtin_amdgcn_global_load_lds(src[j] + static_cast<size_t>(line) * step[j], &lds[stage][q * 64], 16, 0, 0);
+  };
+  auto issue = [&](int stage, int kt) {
+    const int k = kt + rot < nkt ? kt + rot : kt + rot - nkt;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int n = n0 + e / 4 * 8 + lg * 4 + e % 4;
-    if (n < N) stf(out + static_cast<size_t>(m) * N + n, acc[e]);
+    for (int j = 0; j < S::L; ++j) issue_one(stage, k, j);
+    if (S::LR > 0 && wave < S::LR) issue_one(stage, k, S::L);
+  };
+  auto wait_steps = [&](auto steps) {
+    constexpr int n = decltype(steps)::value;
+    if (S::LR > 0 && wave < S::LR) wait_vmcnt_lds<n * (S::L + 1)>();
+    else wait_vmcnt_lds<n * S::L>();
+  };
+
+  f32x4 acc[RB][NB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s)
+    if (s < nkt) issue(s, s);
+  int stage = 0;
+  for (int kt = 0; kt < nkt; ++kt) {
+    // the loads of stage kt have landed; the younger stages, at most NST - 2, stay in flight
+    const int rem = nkt - 1 - kt;
+    if (rem >= NST - 2) wait_steps(std::integral_constant<int, NST - 2>{});
+    else if (NST > 7 && rem == 5) wait_steps(std::integral_constant<int, 5>{});
+    else if (NST > 6 && rem == 4) wait_steps(std::integral_constant<int, 4>{});
+    else if (NST > 5 && rem == 3) wait_steps(std::integral_constant<int, 3>{});
+    else if (NST > 4 && rem == 2) wait_steps(std::integral_constant<int, 2>{});
+    else if (NST > 3 && rem == 1) wait_steps(std::integral_constant<int, 1>{});
+    else wait_steps(std::integral_constant<int, 0>{});
+    __builtin_amdgcn_s_barrier();
+    const int nxt = stage == 0 ? NST - 1 : stage - 1;
+    if (kt + NST - 1 < nkt) issue(nxt, kt + NST - 1);
+    const int k = kt + rot < nkt ? kt + rot : kt + rot - nkt;
+    if (k * SS + kk / 2 < lines) {  // (wavefront-uniform)
+      const uint4* base = &lds[stage][kk / 2 * R * 8];
+      // the scale of block kk % 2 * 4 + lg of a line's eight: bytes [lg % 2][row][kk % 2 * 2 + lg / 2] of its unit
+      const uint8_t* scale = reinterpret_cast<const uint8_t*>(&lds[stage][S::kCodes + kk / 2 * S::UL * 64]) + lg % 2 * 64 + ln * 4 + kk % 2 * 2 + lg / 2;
+      const int c = kk % 2 * 4 + lg;
+      i32x8 af[RB], bf[NB];
+      int as[RB], bs[NB];
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        const int r = (wr * RB + i) * 16 + ln;
+        af[i] = operand(base[r * 8 + (c ^ (r % 8))]);
+        as[i] = scale[(wr * RB + i) * 128];
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int r = BM + j * 16 + ln;
+        bf[j] = operand(base[r * 8 + (c ^ (r % 8))]);
+        bs[j] = scale[(BM / 16 + j) * 128];
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bf[j], af[i], acc[i][j], 4, 4, 0, bs[j], 0, as[i]);
+    }
+    stage = stage + 1 < NST ? stage + 1 : 0;
   }
+  // hand-over: the sums of the wavefronts that shared a row group, added by RG * RB * NB / 8 blocks per wavefront
+  __syncthreads();
+  f32x4* red = reinterpret_cast<f32x4*>(&lds[0][0]);
+  static_assert(8 * RB * NB * 64 <= NST * S::kStage, "hand-over fits the ring");
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) red[((kk * RG + wr) * RB * NB + i * NB + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int x = wave; x < RG * RB * NB; x += 8) {  // block x = (row group, i, j)
+    f32x4 sum = red[x * 64 + lane];
+#pragma unroll
+    for (int v = 1; v < S::KW; ++v) sum += red[(v * RG * RB * NB + x) * 64 + lane];
+    const int j = x % NB, rb = x / NB;
+    const int m = m0 + rb * 16 + ln, n = n0 + j * 16 + lg * 4;
+    if (m >= M || n >= N) continue;
+    const bool whole = n + 4 <= N && N % 4 == 0;
+    if (gridDim.z == 1) store4(out + static_cast<size_t>(m) * N + n, n, N, whole, sum[0], sum[1], sum[2], sum[3]);
+    else store4(sums + (static_cast<size_t>(blockIdx.z) * M + m) * N + n, n, N, whole, sum[0], sum[1], sum[2], sum[3]);
+  }
+}
+
+template <typename T, int RG, int RB, int NB>
+__global__ __launch_bounds__(512) void k_mx4_ring(Mx4Tensor a, Mx4Tensor w, int per_slice, T* __restrict__ out, float* __restrict__ sums) {
+  mx4_ring_body<T, RG, RB, NB>(a, w, per_slice, out, sums);
+}
+
+// out = sum of S slices, in their order
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ sums, int S, long long all, T* __restrict__ out) {
+  for (long long p = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; p < all; p += static_cast<long long>(gridDim.x) * 256) {
+    float v = sums[p];
+    for (int s = 1; s < S; ++s) v += sums[s * all + p];
+    stf(out + p, v);
+  }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------
+// k_mx4_wide<MI, NJ>: tile = 64 MI rows x 64 NJ columns, four wavefronts, one per SIMD, of 32 MI x 32 NJ results each, in 32 x 32 x 64
+// products (9.3 PFLOP/s on zeros with a wavefront per SIMD, 6.6 on random operands; 16 x 16 x 128 5.3 and 5.0: their issue takes longer).
+// A step is 128 bytes, 256 elements, of every row.  Operands, rings and the order of reads and loads are k_gemm_wide's; a step's
+// scales are a load of their own per wavefront (16 groups of 32 rows' 256 bytes, of rows first, then columns) and travel with the ring of X.
+template <int BM, int BN> struct Mx4Rings {
+  static constexpr int kRoom = (160 * 1024 - 4 * 4096) / 128;  // rows of 128 bytes, beside four stages of scales
+  static constexpr int kWhole = kRoom / (BM + BN);
+  static constexpr int kLeft = kRoom - kWhole * (BM + BN);
+  static constexpr int DA0 = kWhole + (kLeft >= BM && (BM >= BN || kLeft < BN) ? 1 : 0);
+  static constexpr int DB0 = kWhole + (DA0 == kWhole && kLeft >= BN ? 1 : 0);
+  static constexpr int DA = DA0 < 4 ? DA0 : 4, DB = DB0 < 4 ? DB0 : 4;
+};
+
+template <typename T, int MI, int NJ>
+__device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tensor& w, T* __restrict__ out) {
+  constexpr int BM = 64 * MI, BN = 64 * NJ, LA = BM / 32, LB = BN / 32;
+  typedef Mx4Rings<BM, BN> Ring;
+  // X, the operand with the shallower ring, has its next block loaded in the second half of a step, Y in the first half of the
+  // next one; the barrier stands between the halves
+  constexpr int DA = Ring::DA, DB = Ring::DB;
+  constexpr bool XB = DA >= DB;
+  constexpr int DX = XB ? DB : DA, DY = XB ? DA : DB, LX = (XB ? LB : LA) + 1, LY = XB ? LA : LB;
+  constexpr int kSlotA = BM * 8, kSlotB = BN * 8, kScales = DA * kSlotA + DB * kSlotB;
+  static_assert((kScales + DX * 256) * sizeof(uint4) <= 160 * 1024 && DX >= 2 && DY <= DX + 1, "LDS of one CU");
+  __shared__ __attribute__((aligned(1024))) uint4 lds[kScales + DX * 256];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int ln = lane % 32, lg = lane / 32;
+  const int wm = wave / 2, wn = wave % 2;
+  const int M = a.rows, N = w.rows, row_bytes = a.Kp / 2, nkt = a.Kp / 256;
+  int col_tile, row_tile;
+  xcd_tile_map_blocked(col_tile, row_tile);
+  const int m0 = row_tile * BM, n0 = col_tile * BN;
+
+  // loader: wavefront v issues instructions L v .. L v + L - 1 of an operand, 8 rows each: a scalar base and a lane offset
+  // (rows past the last one: the last one), and one of the scales, four groups
+  const char *abase[LA], *bbase[LB];
+  uint32_t aoff[LA], boff[LB];
+  const int chunk = ((lane % 8) ^ (lane / 8)) * 16;
+#pragma unroll
+  for (int j = 0; j < LA; ++j) {
+    const int r = min(m0 + 8 * (LA * wave + j), M - 1);
+    abase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(a.codes + static_cast<size_t>(r) * row_bytes));
+    aoff[j] = static_cast<uint32_t>(min(lane / 8, M - 1 - r) * row_bytes + chunk);
+  }
+#pragma unroll
+  for (int j = 0; j < LB; ++j) {
+    const int r = min(n0 + 8 * (LB * wave + j), N - 1);
+    bbase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(w.codes + static_cast<size_t>(r) * row_bytes));
+    boff[j] = static_cast<uint32_t>(min(lane / 8, N - 1 - r) * row_bytes + chunk);
+  }
+  const int group = min(wave * 4 + lane / 16, (BM + BN) / 32 - 1);
+  const bool of_a = group < BM / 32;
+  const int g32 = min(of_a ? m0 / 32 + group : n0 / 32 + group - BM / 32, ((of_a ? M : N) - 1) / 32);
+  const uint8_t* ssrc = (of_a ? a.scales : w.scales) + static_cast<size_t>(g32) * nkt * 256 + lane % 16 * 16;
+  const int rot = (((blockIdx.x + gridDim.x * blockIdx.y) & 7) * nkt) >> 3;  // the walk starts at a step that depends on the XCD
+  auto kof = [&](int kt) { const int k = kt + rot; return k < nkt ? k : k - nkt; };
+  auto issue_a = [&](int slot, int k, int j) {
+    uint32_t o = aoff[j];
+    asm volatile("" : "+v"(o));
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(wave_uniform_ptr(abase[j] + k * 128) + o),
+                                     &lds[slot * kSlotA + (LA * wave + j) * 64], 16, 0, 0);
+  };
+  auto issue_b = [&](int slot, int k, int j) {
+    uint32_t o = boff[j];
+    asm volatile("" : "+v"(o));
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(wave_uniform_ptr(bbase[j] + k * 128) + o),
+                                     &lds[DA * kSlotA + slot * kSlotB + (LB * wave + j) * 64], 16, 0, 0);
+  };
+  auto issue_x = [&](int slot, int k, int j) {
+    if (j == LX - 1) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(ssrc + k * 256), &lds[kScales + slot * 256 + wave * 64], 16, 0, 0);
+    else if (XB) issue_b(slot, k, j);
+    else issue_a(slot, k, j);
+  };
+  auto issue_y = [&](int slot, int k, int j) { if (XB) issue_a(slot, k, j); else issue_b(slot, k, j); };
+  auto block_x = [&](int t) {
+    if (t >= nkt) return;
+    const int k = kof(t);
+#pragma unroll
+    for (int j = 0; j < LX; ++j) issue_x(t, k, j);
+  };
+  auto block_y = [&](int t) {
+    if (t >= nkt) return;
+    const int k = kof(t);
+#pragma unroll
+    for (int j = 0; j < LY; ++j) issue_y(t, k, j);
+  };
+  // in the order of the main loop: X(t), Y(t + DY - DX); Y(DY - 1) goes out in step 0
+#pragma unroll
+  for (int t = 0; t < DY - DX; ++t) block_y(t);
+#pragma unroll
+  for (int t = 0; t < DX - 1; ++t) {
+    block_x(t);
+    block_y(t + DY - DX);
+  }
+  block_x(DX - 1);
+  f32x16 acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  // fragments of a half step: two products' 64 elements each
+  uint4 af[2][2][MI], bf[2][2][NJ];
+  int as[2][MI], bs[2][NJ];  // scales of this step and of the next one
+  auto read = [&](int slot_a, int slot_b, int half, int q) {
+    const int s = q / (MI + NJ), x = q % (MI + NJ), c = (half * 2 + s) * 2 + lg;
+    if (x < NJ) {
+      const int r = wn * (NJ * 32) + x * 32 + ln;
+      bf[half][s][x] = lds[DA * kSlotA + slot_b * kSlotB + r * 8 + (c ^ (r % 8))];
+    } else {
+      const int r = wm * (MI * 32) + (x - NJ) * 32 + ln;
+      af[half][s][x - NJ] = lds[slot_a * kSlotA + r * 8 + (c ^ (r % 8))];
+    }
+  };
+  auto read_scales = [&](int slot_x, int to) {
+    const int* s = reinterpret_cast<const int*>(&lds[kScales + slot_x * 256]) + lane;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) as[to][i] = s[(wm * MI + i) * 64];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) bs[to][j] = s[(2 * MI + wn * NJ + j) * 64];
+  };
+  constexpr int kReads = 2 * (MI + NJ), kMfma = 2 * MI * NJ;
+  constexpr int kSpan = kMfma * 3 / 4;  // MFMAs that reads and loads are spread over
+  auto half_step = [&](auto half_, auto&& between) {
+    constexpr int half = decltype(half_)::value;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          acc[i][j] = half * 2 + s == 0   ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 0, bs[0][j], 0, as[0][i])
+                      : half * 2 + s == 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 1, bs[0][j], 1, as[0][i])
+                      : half * 2 + s == 2 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 2, bs[0][j], 2, as[0][i])
+                                          : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 3, bs[0][j], 3, as[0][i]);
+          __builtin_amdgcn_sched_barrier(0);
+          between((s * MI + i) * NJ + j);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+  };
+  if (nkt >= DY) wait_vmcnt_lds<(DX - 1) * LX + (DY > DX ? DX - 1 : DX - 2) * LY>();
+  else wait_vmcnt_lds<0>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int q = 0; q < kReads; ++q) read(0, 0, 0, q);
+  read_scales(0, 0);
+  int s_a = 0, s_b = 0, s_y = DY - 1;
+  // step kt with `left` steps to come (DX: that many or more)
+  auto step = [&](int kt, auto left_) {
+    constexpr int left = decltype(left_)::value;
+    constexpr int kFly = left == 0 ? 0 : (DX - 2 < left - 1 ? DX - 2 : left - 1) * LX + (DY - 2 < left - 1 ? DY - 2 : left - 1) * LY;
+    const int a1 = s_a + 1 < DA ? s_a + 1 : 0, b1 = s_b + 1 < DB ? s_b + 1 : 0;
+    const int ky = left >= DY - 1 ? kof(kt + DY - 1) : 0, kx = left >= DX ? kof(kt + DX) : 0;
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+    half_step(std::integral_constant<int, 0>{}, [&](int t) {
+#pragma unroll
+      for (int q = 0; q < kReads; ++q)
+        if (1 + q * kSpan / kReads == t) read(s_a, s_b, 1, q);
+#pragma unroll
+      for (int l = 0; l < LY; ++l)
+        if (left >= DY - 1 && l * kSpan / LY == t) issue_y(s_y, ky, l);
+    });
+    wait_vmcnt_lds<kFly>();
+    if (left > 0) __builtin_amdgcn_s_barrier();
+    half_step(std::integral_constant<int, 1>{}, [&](int t) {
+      if (left > 0 && t == 0) read_scales(XB ? b1 : a1, 1);
+#pragma unroll
+      for (int q = 0; q < kReads; ++q)
+        if (left > 0 && 1 + q * kSpan / kReads == t) read(a1, b1, 0, q);
+#pragma unroll
+      for (int l = 0; l < LX; ++l)
+        if (left >= DX && l * kSpan / LX == t) issue_x(XB ? s_b : s_a, kx, l);
+    });
+    if (left > 0) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) as[0][i] = as[1][i];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) bs[0][j] = bs[1][j];
+    }
+    s_y = XB ? s_a : s_b;
+    s_a = a1;
+    s_b = b1;
+  };
+  int kt = 0;
+  for (; kt < nkt - DX; ++kt) step(kt, std::integral_constant<int, DX>{});
+  if constexpr (DX > 3) { if (nkt - kt > 3) step(kt++, std::integral_constant<int, 3>{}); }
+  if constexpr (DX > 2) { if (nkt - kt > 2) step(kt++, std::integral_constant<int, 2>{}); }
+  if (nkt - kt > 1) step(kt++, std::integral_constant<int, 1>{});
+  step(kt, std::integral_constant<int, 0>{});
+  // a lane: row ln of block i, columns 8 q + 4 lg .. + 3 of block j
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int m = m0 + wm * (MI * 32) + i * 32 + ln;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = n0 + wn * (NJ * 32) + j * 32 + q * 8 + lg * 4;
+        if (m < M && n < N)
+          store4(out + static_cast<size_t>(m) * N + n, n, N, N % 4 == 0, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                 acc[i][j][4 * q + 3]);
+      }
+  }
+}
+
+template <typename T, int MI, int NJ>
+__global__ __launch_bounds__(256, 1) void k_mx4_wide(Mx4Tensor a, Mx4Tensor w, T* __restrict__ out) {
+  mx4_wide_body<T, MI, NJ>(a, w, out);
 }
 
 inline bool whole_pieces(const void* p, int K) { return K % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -137,12 +498,88 @@ void launch_load8(int dtype, const int8_t* q, const float* scale, int q_rows, in
 #undef DLLMC_CALL
 }
 
-size_t linear_mx4_scratch_bytes(int, int, int) { return 0; }
+namespace {
 
-void launch_linear_mx4(int dtype, Mx4Tensor a, Mx4Tensor w, void* out, void*, hipStream_t st) {
-  const dim3 grid(((w.rows + 127) / 128) * ((a.rows + 31) / 32));
-  if (dtype == 1) hipLaunchKernelGGL(k_mx4_plain<bf16_t>, grid, dim3(256), 0, st, a, w, static_cast<bf16_t*>(out));
-  else hipLaunchKernelGGL(k_mx4_plain<float>, grid, dim3(256), 0, st, a, w, static_cast<float*>(out));
+// Tile and slices with the lowest estimate, us: start + rounds of 256 workgroups x (round + line x 128-byte lines) + MB of weights x w + MB of
+// results x out, or of float32 sums x sums + the launch that adds them.
+struct Mx4Cost { int wide, bm, bn; double start, round, line, w, out, sums, add; };
+constexpr Mx4Cost kMx4Costs[] = {
+    {0, 16, 16, 1.5, 1.3, 0.07, 0.058, 1.0, 0.6, 2.5}, {0, 16, 48, 1.5, 1.5, 0.10, 0.08, 0.9, 0.6, 2.5}, {0, 32, 32, 1.8, 1.4, 0.12, 0.06, 0.3, 0.6, 2.5},
+    {0, 32, 64, 1.4, 2.1, 0.18, 0.06, 0.25, 0.5, 2.5}, {0, 64, 32, 1.9, 1.2, 0.19, 0.03, 0.9, 0.6, 2.5},  {0, 64, 48, 2.2, 1.4, 0.22, 0.05, 0.7, 0.6, 2.5},
+    {0, 64, 80, 2.4, 1.5, 0.30, 0.03, 0.8, 0.6, 2.5},  {0, 128, 64, 2.9, 1.7, 0.36, 0.03, 0.5, 0.6, 2.5}, {1, 128, 64, 1.6, 1.9, 0.35, 0.04, 0.2, 0, 0},
+    {1, 128, 128, 1.6, 3.1, 0.5, 0.05, 0.22, 0, 0},     {1, 128, 256, 1.4, 5.6, 0.8, 0.03, 0.21, 0, 0},   {1, 192, 128, 0.6, 5.0, 0.6, 0.02, 0.3, 0, 0},
+    {1, 192, 256, 0, 8.8, 0.95, 0.02, 0.26, 0, 0},     {1, 256, 128, 1.8, 4.3, 0.72, 0.005, 0.39, 0, 0},  {1, 256, 256, 0.8, 9.6, 1.2, 0.005, 0.3, 0, 0}};
+
+template <typename T>
+void launch_product(const Mx4Plan& p, Mx4Tensor a, Mx4Tensor w, T* out, float* sums, hipStream_t st) {
+  const dim3 grid((w.rows + p.bn - 1) / p.bn, (a.rows + p.bm - 1) / p.bm, p.S);
+  if (p.wide) {
+#define DLLMC_W(MI, NJ) hipLaunchKernelGGL((k_mx4_wide<T, MI, NJ>), grid, dim3(256), 0, st, a, w, out)
+    switch (p.bm * 1000 + p.bn) {
+      case 256256: DLLMC_W(4, 4); break;
+      case 192256: DLLMC_W(3, 4); break;
+      case 256128: DLLMC_W(4, 2); break;
+      case 128256: DLLMC_W(2, 4); break;
+      case 192128: DLLMC_W(3, 2); break;
+      case 128128: DLLMC_W(2, 2); break;
+      default: DLLMC_W(2, 1); break;
+    }
+#undef DLLMC_W
+    return;
+  }
+#define DLLMC_R(RG, RB, NB) hipLaunchKernelGGL((k_mx4_ring<T, RG, RB, NB>), grid, dim3(512), 0, st, a, w, p.per, out, sums)
+  switch (p.bm * 100 + p.bn) {
+    case 1616: DLLMC_R(1, 1, 1); break;
+    case 1648: DLLMC_R(1, 1, 3); break;
+    case 3232: DLLMC_R(1, 2, 2); break;
+    case 3264: DLLMC_R(1, 2, 4); break;
+    case 6432: DLLMC_R(2, 2, 2); break;
+    case 6448: DLLMC_R(2, 2, 3); break;
+    case 6480: DLLMC_R(2, 2, 5); break;
+    default: DLLMC_R(2, 4, 4); break;
+  }
+#undef DLLMC_R
+  if (p.S > 1) {
+    const long long all = static_cast<long long>(a.rows) * w.rows, g = (all + 255) / 256;
+    hipLaunchKernelGGL(k_mx4_sum<T>, dim3(static_cast<unsigned>(g < (1 << 20) ? g : 1 << 20)), dim3(256), 0, st, sums, p.S, all, out);
+  }
+}
+
+Mx4Plan choose_mx4(int M, int N, int Kp) {
+  const int lines = Kp / 256;
+  const double mb_w = static_cast<double>(N) * Kp / 2e6, mn = static_cast<double>(M) * N / 1e6;
+  Mx4Plan best{};
+  double best_t = 1e300;
+  for (const Mx4Cost& c : kMx4Costs) {
+    const long long mt = (M + c.bm - 1) / c.bm, nt = (N + c.bn - 1) / c.bn;
+    if (mt > 65535) continue;  // (the grid's second dimension)
+    for (const int S : {1, 2, 3, 4, 6, 8}) {
+      if (S > 1 && (c.wide || S > lines)) break;
+      const int per = (lines + S - 1) / S, used = (lines + per - 1) / per;
+      const double rounds = static_cast<double>((mt * nt * used + 255) / 256);
+      const double t = c.start + rounds * (c.round + c.line * per) + mb_w * c.w + (used == 1 ? 2 * mn * c.out : used * 4 * mn * c.sums + c.add);
+      if (t < best_t) {
+        best_t = t;
+        best = {c.wide, c.bm, c.bn, used, per};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace
+
+Mx4Plan plan_mx4(int M, int N, int Kp) {
+  return last_plan<Mx4Plan>({M, N, Kp}, [&] { return choose_mx4(M, N, Kp); });
+}
+
+size_t linear_mx4_scratch_bytes(const Mx4Plan& p, int M, int N) {
+  return p.S == 1 ? 0 : static_cast<size_t>(p.S) * M * N * sizeof(float);
+}
+
+void launch_linear_mx4(const Mx4Plan& p, int dtype, Mx4Tensor a, Mx4Tensor w, void* out, void* scratch, hipStream_t st) {
+  if (dtype == 1) launch_product(p, a, w, static_cast<bf16_t*>(out), static_cast<float*>(scratch), st);
+  else launch_product(p, a, w, static_cast<float*>(out), static_cast<float*>(scratch), st);
 }
 
 }  // namespace dllmc

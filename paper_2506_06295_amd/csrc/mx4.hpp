@@ -82,8 +82,10 @@ template <bool VEC, typename T> __device__ __forceinline__ void store8(T* row, i
 void launch_quant_mx4(int dtype, const void* x, int x_rows, const int* rows, int M, int K, Mx4Tensor out, hipStream_t st);
 void launch_mx4_load(int dtype, Mx4Tensor in, const int* rows, int M, int K, void* out, hipStream_t st);
 void launch_load8(int dtype, const int8_t* q, const float* scale, int q_rows, int K, const int* rows, int M, void* out, hipStream_t st);
-size_t linear_mx4_scratch_bytes(int M, int N, int Kp);
-void launch_linear_mx4(int dtype, Mx4Tensor a, Mx4Tensor w, void* out, void* scratch, hipStream_t st);
+struct Mx4Plan { int wide, bm, bn, S, per; };  // wide: tile kernel; else ring of bm x bn and S slices of `per` lines of 256 elements
+Mx4Plan plan_mx4(int M, int N, int Kp);
+size_t linear_mx4_scratch_bytes(const Mx4Plan& p, int M, int N);
+void launch_linear_mx4(const Mx4Plan& p, int dtype, Mx4Tensor a, Mx4Tensor w, void* out, void* scratch, hipStream_t st);
 
 // Norm of stream + x in few bits (kernels_norm8.hip): 8-bit rows (q, scale) or 4-bit ones (mx).
 struct NormRows {

@@ -35,7 +35,7 @@ def test_sizes():
         binding.mx4_bytes(1 << 40, 32)
     for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), ((1 << 22) + 1, 1, 1), (1, 1, 131073), (1 << 18, (1 << 17) + 1, 64)):
         assert L.dllmc_op_linear_mx4_scratch_bytes(*bad) == 0
-    for bad in ((2, 1, 1, 1), (F32, 0, 1, 1), (F32, 1 << 24, 1, 1), (F32, 1, 0, 1), (F32, 1, 1 << 25, 1), (F32, 1, 1, 65), (F32, 1, 1, -1)):
+    for bad in ((2, 1, 1, 1), (F32, 0, 1, 1), (F32, 1 << 23, 1, 1), (F32, 1 << 22, 1 << 19, 1), (F32, 1, 0, 1), (F32, 1, 1 << 25, 1), (F32, 1, 1, 65), (F32, 1, 1, -1)):
         assert L.dllmc_op_logprobs_scratch_bytes(*bad) == 0
 
 
@@ -76,7 +76,7 @@ BAD = {
     "dllmc_op_linear_mx4": [dict(dtype=2), dict(a=None), dict(w=None), dict(out=None), dict(M=0), dict(N=0), dict(K=0), dict(K=131073),
                             dict(M=(1 << 22) + 1), dict(N=(1 << 24) + 1), dict(M=1 << 18, N=(1 << 17) + 1), dict(a=near(p(0), 8)),
                             dict(w=near(p(1), 4)), dict(out=near(p(2), 8)), dict(scratch=near(p(3), 8)), dict(out=p(0)), dict(out=p(1))],
-    "dllmc_op_logprobs": [dict(dtype=2), dict(logits=None), dict(ld=99), dict(M=0), dict(M=1 << 24), dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25),
+    "dllmc_op_logprobs": [dict(dtype=2), dict(logits=None), dict(ld=99), dict(M=0), dict(M=1 << 23), dict(M=1 << 22, vocab=1 << 19, ld=1 << 19), dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25),
                           dict(n=-1), dict(n=0), dict(n=65537), dict(k=-1), dict(k=0), dict(k=65), dict(tokens=None), dict(logp=None),
                           dict(ids=None), dict(top=None), dict(n=0, tokens=None, logp=None, k=0, ids=None, top=None, entropy=None),
                           dict(logits=near(p(0), 1)), dict(tokens=near(p(1), 2)), dict(logp=near(p(2), 2)), dict(entropy=near(p(3), 2)),
