@@ -11,6 +11,7 @@ namespace dllmc {
 
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -71,9 +72,10 @@ __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, con
 // ---- the product ------------------------------------------------------------------------------------------
 // Products are taken as W A^T, so that a lane holds neighbouring columns of a row.  Rows past M and N repeat the last one (their scales are those
 // of the last rows' group) and are dropped at the store.
-__device__ __forceinline__ i32x8 operand(const uint4& u) {  // (a 4-bit operand is the first four registers)
-  return i32x8{static_cast<int>(u.x), static_cast<int>(u.y), static_cast<int>(u.z), static_cast<int>(u.w), 0, 0, 0, 0};
-}
+// (A 4-bit operand is the first four registers.  LDS is read as i32x4: before a copied struct the compiler waits for every load into LDS.)
+__device__ __forceinline__ i32x8 operand(const i32x4& u) { return i32x8{u[0], u[1], u[2], u[3], 0, 0, 0, 0}; }
+
+typedef const __attribute__((address_space(1))) int* global_int_ptr;  // (a pointer put together from registers: a flat load otherwise)
 
 // four neighbouring results of a row, n0 + 4 <= N or element by element
 template <typename T>
@@ -198,13 +200,13 @@ __device__ __forceinline__ void mx4_ring_body(const Mx4Tensor& a, const Mx4Tenso
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
         const int r = (wr * RB + i) * 16 + ln;
-        af[i] = operand(base[r * 8 + (c ^ (r % 8))]);
+        af[i] = operand(__builtin_bit_cast(i32x4, base[r * 8 + (c ^ (r % 8))]));
         as[i] = scale[(wr * RB + i) * 128];
       }
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const int r = BM + j * 16 + ln;
-        bf[j] = operand(base[r * 8 + (c ^ (r % 8))]);
+        bf[j] = operand(__builtin_bit_cast(i32x4, base[r * 8 + (c ^ (r % 8))]));
         bs[j] = scale[(BM / 16 + j) * 128];
       }
 #pragma unroll
@@ -255,10 +257,13 @@ __global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ sums,
 // ---- many rows ----------------------------------------------------------------------------------------
 // k_mx4_wide<MI, NJ>: tile = 64 MI rows x 64 NJ columns, four wavefronts, one per SIMD, of 32 MI x 32 NJ results each, in 32 x 32 x 64
 // products (9.3 PFLOP/s on zeros with a wavefront per SIMD, 6.6 on random operands; 16 x 16 x 128 5.3 and 5.0: their issue takes longer).
-// A step is 128 bytes, 256 elements, of every row.  Operands, rings and the order of reads and loads are k_gemm_wide's; a step's
-// scales are a load of their own per wavefront (16 groups of 32 rows' 256 bytes, of rows first, then columns) and travel with the ring of X.
+// A step is 128 bytes, 256 elements, of every row.  Operands, rings and the order of reads and loads are k_gemm_wide's.  A step's scales
+// are one more load of every wavefront (16 groups of 32 rows' 256 bytes, of rows first, then columns) and travel with the ring of X; the tile of
+// 256 x 256 fills LDS (two stages of each operand instead would leave Y half a step to land), and its wavefronts load their own blocks' scales
+// into registers, a step ahead.
 template <int BM, int BN> struct Mx4Rings {
-  static constexpr int kRoom = (160 * 1024 - 4 * 4096) / 128;  // rows of 128 bytes, beside four stages of scales
+  static constexpr bool kInLds = BM + BN < 512;
+  static constexpr int kRoom = kInLds ? 1280 - 4 * 32 : 1280;  // rows of 128 bytes, beside four stages of scales
   static constexpr int kWhole = kRoom / (BM + BN);
   static constexpr int kLeft = kRoom - kWhole * (BM + BN);
   static constexpr int DA0 = kWhole + (kLeft >= BM && (BM >= BN || kLeft < BN) ? 1 : 0);
@@ -273,11 +278,11 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
   // X, the operand with the shallower ring, has its next block loaded in the second half of a step, Y in the first half of the
   // next one; the barrier stands between the halves
   constexpr int DA = Ring::DA, DB = Ring::DB;
-  constexpr bool XB = DA >= DB;
-  constexpr int DX = XB ? DB : DA, DY = XB ? DA : DB, LX = (XB ? LB : LA) + 1, LY = XB ? LA : LB;
-  constexpr int kSlotA = BM * 8, kSlotB = BN * 8, kScales = DA * kSlotA + DB * kSlotB;
-  static_assert((kScales + DX * 256) * sizeof(uint4) <= 160 * 1024 && DX >= 2 && DY <= DX + 1, "LDS of one CU");
-  __shared__ __attribute__((aligned(1024))) uint4 lds[kScales + DX * 256];
+  constexpr bool XB = DA >= DB, kInLds = Ring::kInLds;
+  constexpr int DX = XB ? DB : DA, DY = XB ? DA : DB, LX = (XB ? LB : LA) + (kInLds ? 1 : 0), LY = XB ? LA : LB;
+  constexpr int kSlotA = BM * 8, kSlotB = BN * 8, kScales = DA * kSlotA + DB * kSlotB, kLds = kScales + (kInLds ? DX * 256 : 0);
+  static_assert(kLds * sizeof(uint4) <= 160 * 1024 && DX >= 2 && DY <= DX + 1, "LDS of one CU");
+  __shared__ __attribute__((aligned(1024))) uint4 lds[kLds];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int ln = lane % 32, lg = lane / 32;
   const int wm = wave / 2, wn = wave % 2;
@@ -287,8 +292,8 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
   const int m0 = row_tile * BM, n0 = col_tile * BN;
 
   // loader: wavefront v issues instructions L v .. L v + L - 1 of an operand, 8 rows each: a scalar base and a lane offset
-  // (rows past the last one: the last one), and one of the scales, four groups
-  const char *abase[LA], *bbase[LB];
+  // (rows past the last one: the last one; groups of scales likewise)
+  const char *abase[LA], *bbase[LB], *asbase[MI], *bsbase[NJ];
   uint32_t aoff[LA], boff[LB];
   const int chunk = ((lane % 8) ^ (lane / 8)) * 16;
 #pragma unroll
@@ -303,10 +308,17 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     bbase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(w.codes + static_cast<size_t>(r) * row_bytes));
     boff[j] = static_cast<uint32_t>(min(lane / 8, N - 1 - r) * row_bytes + chunk);
   }
+  // scales: in LDS one load of four groups a wavefront, else one of a group for each of its blocks
   const int group = min(wave * 4 + lane / 16, (BM + BN) / 32 - 1);
   const bool of_a = group < BM / 32;
   const int g32 = min(of_a ? m0 / 32 + group : n0 / 32 + group - BM / 32, ((of_a ? M : N) - 1) / 32);
   const uint8_t* ssrc = (of_a ? a.scales : w.scales) + static_cast<size_t>(g32) * nkt * 256 + lane % 16 * 16;
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+    asbase[i] = wave_uniform_ptr(reinterpret_cast<const char*>(a.scales) + static_cast<size_t>(min(m0 / 32 + wm * MI + i, (M - 1) / 32)) * nkt * 256);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+    bsbase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(w.scales) + static_cast<size_t>(min(n0 / 32 + wn * NJ + j, (N - 1) / 32)) * nkt * 256);
   const int rot = (((blockIdx.x + gridDim.x * blockIdx.y) & 7) * nkt) >> 3;  // the walk starts at a step that depends on the XCD
   auto kof = [&](int kt) { const int k = kt + rot; return k < nkt ? k : k - nkt; };
   auto issue_a = [&](int slot, int k, int j) {
@@ -322,24 +334,44 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
                                      &lds[DA * kSlotA + slot * kSlotB + (LB * wave + j) * 64], 16, 0, 0);
   };
   auto issue_x = [&](int slot, int k, int j) {
-    if (j == LX - 1) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(ssrc + k * 256), &lds[kScales + slot * 256 + wave * 64], 16, 0, 0);
+    if (kInLds && j == LX - 1)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(ssrc + k * 256), &lds[kInLds ? kScales + slot * 256 + wave * 64 : 0], 16, 0, 0);
     else if (XB) issue_b(slot, k, j);
     else issue_a(slot, k, j);
   };
   auto issue_y = [&](int slot, int k, int j) { if (XB) issue_a(slot, k, j); else issue_b(slot, k, j); };
+  int as[2][MI], bs[2][NJ];  // scales of this step and of the next one
+  auto read_scales = [&](int slot_x, int to) {
+    const int* s = reinterpret_cast<const int*>(&lds[kInLds ? kScales + slot_x * 256 : 0]) + lane;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) as[to][i] = s[(wm * MI + i) * 64];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) bs[to][j] = s[(2 * MI + wn * NJ + j) * 64];
+  };
+  auto load_scales = [&](int to, int k) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) as[to][i] = reinterpret_cast<global_int_ptr>(reinterpret_cast<uintptr_t>(wave_uniform_ptr(asbase[i] + k * 256)))[lane];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) bs[to][j] = reinterpret_cast<global_int_ptr>(reinterpret_cast<uintptr_t>(wave_uniform_ptr(bsbase[j] + k * 256)))[lane];
+  };
+  // The first blocks in the order of the main loop: X(t), Y(t + DY - DX); Y(DY - 1) goes out in step 0.  Straight code, whatever nkt is (a
+  // step that there is not: the last one's block again, which nobody reads): over loads that may or may not have been issued the
+  // compiler would wait for the scales in every step.
   auto block_x = [&](int t) {
-    if (t >= nkt) return;
-    const int k = kof(t);
+    const int k = kof(min(t, nkt - 1));
 #pragma unroll
     for (int j = 0; j < LX; ++j) issue_x(t, k, j);
   };
   auto block_y = [&](int t) {
-    if (t >= nkt) return;
-    const int k = kof(t);
+    const int k = kof(min(t, nkt - 1));
 #pragma unroll
     for (int j = 0; j < LY; ++j) issue_y(t, k, j);
   };
-  // in the order of the main loop: X(t), Y(t + DY - DX); Y(DY - 1) goes out in step 0
+  if constexpr (!kInLds) {
+    load_scales(0, kof(0));
+    load_scales(1, kof(min(1, nkt - 1)));
+    __builtin_amdgcn_sched_barrier(0);
+  }
 #pragma unroll
   for (int t = 0; t < DY - DX; ++t) block_y(t);
 #pragma unroll
@@ -348,6 +380,8 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     block_y(t + DY - DX);
   }
   block_x(DX - 1);
+  wait_vmcnt_lds<(DX - 1) * LX + (DY > DX ? DX - 1 : DX - 2) * LY>();
+  __builtin_amdgcn_s_barrier();
   f32x16 acc[MI][NJ];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
@@ -355,25 +389,16 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  // fragments of a half step: two products' 64 elements each
-  uint4 af[2][2][MI], bf[2][2][NJ];
-  int as[2][MI], bs[2][NJ];  // scales of this step and of the next one
+  i32x4 af[2][2][MI], bf[2][2][NJ];  // fragments of a half step: two products' 64 elements each
   auto read = [&](int slot_a, int slot_b, int half, int q) {
     const int s = q / (MI + NJ), x = q % (MI + NJ), c = (half * 2 + s) * 2 + lg;
     if (x < NJ) {
       const int r = wn * (NJ * 32) + x * 32 + ln;
-      bf[half][s][x] = lds[DA * kSlotA + slot_b * kSlotB + r * 8 + (c ^ (r % 8))];
+      bf[half][s][x] = __builtin_bit_cast(i32x4, lds[DA * kSlotA + slot_b * kSlotB + r * 8 + (c ^ (r % 8))]);
     } else {
       const int r = wm * (MI * 32) + (x - NJ) * 32 + ln;
-      af[half][s][x - NJ] = lds[slot_a * kSlotA + r * 8 + (c ^ (r % 8))];
+      af[half][s][x - NJ] = __builtin_bit_cast(i32x4, lds[slot_a * kSlotA + r * 8 + (c ^ (r % 8))]);
     }
-  };
-  auto read_scales = [&](int slot_x, int to) {
-    const int* s = reinterpret_cast<const int*>(&lds[kScales + slot_x * 256]) + lane;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) as[to][i] = s[(wm * MI + i) * 64];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) bs[to][j] = s[(2 * MI + wn * NJ + j) * 64];
   };
   constexpr int kReads = 2 * (MI + NJ), kMfma = 2 * MI * NJ;
   constexpr int kSpan = kMfma * 3 / 4;  // MFMAs that reads and loads are spread over
@@ -385,25 +410,23 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          acc[i][j] = half * 2 + s == 0   ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 0, bs[0][j], 0, as[0][i])
-                      : half * 2 + s == 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 1, bs[0][j], 1, as[0][i])
-                      : half * 2 + s == 2 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 2, bs[0][j], 2, as[0][i])
-                                          : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, 3, bs[0][j], 3, as[0][i]);
+#define DLLMC_MFMA(B) \
+  __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(bf[half][s][j]), operand(af[half][s][i]), acc[i][j], 4, 4, B, bs[0][j], B, as[0][i])
+          acc[i][j] = half * 2 + s == 0 ? DLLMC_MFMA(0) : half * 2 + s == 1 ? DLLMC_MFMA(1) : half * 2 + s == 2 ? DLLMC_MFMA(2) : DLLMC_MFMA(3);
+#undef DLLMC_MFMA
           __builtin_amdgcn_sched_barrier(0);
           between((s * MI + i) * NJ + j);
           __builtin_amdgcn_sched_barrier(0);
         }
   };
-  if (nkt >= DY) wait_vmcnt_lds<(DX - 1) * LX + (DY > DX ? DX - 1 : DX - 2) * LY>();
-  else wait_vmcnt_lds<0>();
-  __builtin_amdgcn_s_barrier();
 #pragma unroll
   for (int q = 0; q < kReads; ++q) read(0, 0, 0, q);
-  read_scales(0, 0);
+  if constexpr (kInLds) read_scales(0, 0);
   int s_a = 0, s_b = 0, s_y = DY - 1;
   // step kt with `left` steps to come (DX: that many or more)
   auto step = [&](int kt, auto left_) {
     constexpr int left = decltype(left_)::value;
+    // (the loads of scales are not counted: those behind what has to have landed only make the wait a longer one)
     constexpr int kFly = left == 0 ? 0 : (DX - 2 < left - 1 ? DX - 2 : left - 1) * LX + (DY - 2 < left - 1 ? DY - 2 : left - 1) * LY;
     const int a1 = s_a + 1 < DA ? s_a + 1 : 0, b1 = s_b + 1 < DB ? s_b + 1 : 0;
     const int ky = left >= DY - 1 ? kof(kt + DY - 1) : 0, kx = left >= DX ? kof(kt + DX) : 0;
@@ -420,7 +443,7 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     wait_vmcnt_lds<kFly>();
     if (left > 0) __builtin_amdgcn_s_barrier();
     half_step(std::integral_constant<int, 1>{}, [&](int t) {
-      if (left > 0 && t == 0) read_scales(XB ? b1 : a1, 1);
+      if (kInLds && left > 0 && t == 0) read_scales(XB ? b1 : a1, 1);
 #pragma unroll
       for (int q = 0; q < kReads; ++q)
         if (left > 0 && 1 + q * kSpan / kReads == t) read(a1, b1, 0, q);
@@ -430,9 +453,19 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     });
     if (left > 0) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) as[0][i] = as[1][i];
+      for (int i = 0; i < MI; ++i) {
+        as[0][i] = as[1][i];
+        if (!kInLds) asm volatile("" : "+v"(as[0][i]));  // (the copy first: then the loads go to the registers that the copy has left)
+      }
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) bs[0][j] = bs[1][j];
+      for (int j = 0; j < NJ; ++j) {
+        bs[0][j] = bs[1][j];
+        if (!kInLds) asm volatile("" : "+v"(bs[0][j]));
+      }
+      if (!kInLds) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (left > 1) load_scales(1, kof(kt + 2));
+      }
     }
     s_y = XB ? s_a : s_b;
     s_a = a1;
@@ -444,7 +477,35 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
   if constexpr (DX > 2) { if (nkt - kt > 2) step(kt++, std::integral_constant<int, 2>{}); }
   if (nkt - kt > 1) step(kt++, std::integral_constant<int, 1>{});
   step(kt, std::integral_constant<int, 0>{});
-  // a lane: row ln of block i, columns 8 q + 4 lg .. + 3 of block j
+  // A lane: row ln of block i, columns 8 q + 4 lg .. + 3 of block j.  Stored as they are, 16 bytes of every row at a time, they cost more than
+  // a trip through LDS, 32 rows of the wavefront's columns at a time, that makes whole lines of them (12288 x 12288 x 4096: 45 us of
+  // 320 for the direct stores).  Rows are 16 bytes further apart than they are long: no two lanes meet in a bank.
+  constexpr int kPer = 16 / sizeof(T), kRow = NJ * 32 / kPer;  // elements and slots of 16 bytes
+  constexpr int kPitch = kRow + 1;
+  static_assert(4 * 32 * kPitch <= DA * kSlotA + DB * kSlotB, "results fit the ring");
+  if (N % kPer == 0) {  // (kernel-uniform)
+    __syncthreads();
+    uint4* mine = lds + wave * 32 * kPitch;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          store4(reinterpret_cast<T*>(mine + ln * kPitch) + j * 32 + q * 8 + lg * 4, 0, 4, true, acc[i][j][4 * q], acc[i][j][4 * q + 1],
+                 acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int s = 0; s < 32 * kRow / 64; ++s) {
+        const int at = s * 64 + lane, r = at / kRow, c = at % kRow;
+        const int m = m0 + wm * (MI * 32) + i * 32 + r, n = n0 + wn * (NJ * 32) + c * kPer;
+        const i32x4 v = __builtin_bit_cast(i32x4, mine[r * kPitch + c]);
+        if (m < M && n < N) *reinterpret_cast<i32x4*>(out + static_cast<size_t>(m) * N + n) = v;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int m = m0 + wm * (MI * 32) + i * 32 + ln;
