@@ -562,14 +562,19 @@ void launch_load8(int dtype, const int8_t* q, const float* scale, int q_rows, in
 namespace {
 
 // Tile and slices with the lowest estimate, us: start + rounds of 256 workgroups x (round + line x 128-byte lines) + MB of weights x w + MB of
-// results x out, or of float32 sums x sums + the launch that adds them.
+// results x out, or of float32 sums x sums + the launch that adds them.  Fitted (4 to 9 % rms) to 2300 launches, cold weights, 1 to 12288 rows of
+// thirteen maps of 256 to 126464 outputs; the choices are 1.6 % from the quickest on average.  The shapes are those of 24 without which they
+// would be further: 64 x 12288 x 4096 9.2 us (tiles of 128 x 64; 11.8 of 128 x 128), 1280 x 18944 x 3584 48.8 in two rounds of 256 x 192 (55.6 of
+// 256 x 256, 61.7 of 192 x 256, a third round for six tiles), 1 x 12288 x 4096 7.0 (16 x 48) and 11.1 (16 x 16, three rounds).
 struct Mx4Cost { int wide, bm, bn; double start, round, line, w, out, sums, add; };
 constexpr Mx4Cost kMx4Costs[] = {
-    {0, 16, 16, 1.5, 1.3, 0.07, 0.058, 1.0, 0.6, 2.5}, {0, 16, 48, 1.5, 1.5, 0.10, 0.08, 0.9, 0.6, 2.5}, {0, 32, 32, 1.8, 1.4, 0.12, 0.06, 0.3, 0.6, 2.5},
-    {0, 32, 64, 1.4, 2.1, 0.18, 0.06, 0.25, 0.5, 2.5}, {0, 64, 32, 1.9, 1.2, 0.19, 0.03, 0.9, 0.6, 2.5},  {0, 64, 48, 2.2, 1.4, 0.22, 0.05, 0.7, 0.6, 2.5},
-    {0, 64, 80, 2.4, 1.5, 0.30, 0.03, 0.8, 0.6, 2.5},  {0, 128, 64, 2.9, 1.7, 0.36, 0.03, 0.5, 0.6, 2.5}, {1, 128, 64, 1.6, 1.9, 0.35, 0.04, 0.2, 0, 0},
-    {1, 128, 128, 1.6, 3.1, 0.5, 0.05, 0.22, 0, 0},     {1, 128, 256, 1.4, 5.6, 0.8, 0.03, 0.21, 0, 0},   {1, 192, 128, 0.6, 5.0, 0.6, 0.02, 0.3, 0, 0},
-    {1, 192, 256, 0, 8.8, 0.95, 0.02, 0.26, 0, 0},     {1, 256, 128, 1.8, 4.3, 0.72, 0.005, 0.39, 0, 0},  {1, 256, 256, 0.8, 9.6, 1.2, 0.005, 0.3, 0, 0}};
+    {0, 16, 16, 2.44, 1.23, 0.0843, 0.0361, 0.372, 0, 2.5}, {0, 16, 48, 2.1, 1.46, 0.113, 0.0464, 0.698, 0.608, 2.37},
+    {0, 16, 80, 1.38, 2.33, 0.17, 0.0594, 0, 0.377, 2.23}, {0, 32, 32, 1.99, 1.76, 0.122, 0, 0.144, 0.338, 2.4},
+    {0, 32, 64, 1.16, 2.67, 0.182, 0.0382, 0, 0.439, 2.15}, {0, 64, 64, 1.02, 2.72, 0.269, 0.0261, 0.162, 0.496, 2.39},
+    {0, 64, 80, 1.25, 2.88, 0.299, 0.0406, 0.274, 0.553, 2.26}, {1, 128, 64, 1.52, 1.83, 0.353, 0.0323, 0.0719, 0, 0},
+    {1, 128, 128, 1.56, 1.96, 0.491, 0.0494, 0.156, 0, 0}, {1, 192, 128, 0.989, 3.06, 0.589, 0.0324, 0.139, 0, 0},
+    {1, 192, 256, 0.525, 5, 0.893, 0.0587, 0.156, 0, 0}, {1, 256, 128, 0.236, 4.26, 0.694, 0.0403, 0.131, 0, 0},
+    {1, 256, 192, 0.65, 4.97, 0.88, 0.0502, 0.163, 0, 0}, {1, 256, 256, 0, 6.1, 1.1, 0.0514, 0.177, 0, 0}};
 
 template <typename T>
 void launch_product(const Mx4Plan& p, Mx4Tensor a, Mx4Tensor w, T* out, float* sums, hipStream_t st) {
@@ -580,7 +585,7 @@ void launch_product(const Mx4Plan& p, Mx4Tensor a, Mx4Tensor w, T* out, float* s
       case 256256: DLLMC_W(4, 4); break;
       case 192256: DLLMC_W(3, 4); break;
       case 256128: DLLMC_W(4, 2); break;
-      case 128256: DLLMC_W(2, 4); break;
+      case 256192: DLLMC_W(4, 3); break;
       case 192128: DLLMC_W(3, 2); break;
       case 128128: DLLMC_W(2, 2); break;
       default: DLLMC_W(2, 1); break;
@@ -592,12 +597,11 @@ void launch_product(const Mx4Plan& p, Mx4Tensor a, Mx4Tensor w, T* out, float* s
   switch (p.bm * 100 + p.bn) {
     case 1616: DLLMC_R(1, 1, 1); break;
     case 1648: DLLMC_R(1, 1, 3); break;
+    case 1680: DLLMC_R(1, 1, 5); break;
     case 3232: DLLMC_R(1, 2, 2); break;
     case 3264: DLLMC_R(1, 2, 4); break;
-    case 6432: DLLMC_R(2, 2, 2); break;
-    case 6448: DLLMC_R(2, 2, 3); break;
-    case 6480: DLLMC_R(2, 2, 5); break;
-    default: DLLMC_R(2, 4, 4); break;
+    case 6464: DLLMC_R(2, 2, 4); break;
+    default: DLLMC_R(2, 2, 5); break;
   }
 #undef DLLMC_R
   if (p.S > 1) {
