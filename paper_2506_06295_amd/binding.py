@@ -894,7 +894,8 @@ def op_mx4_load(dtype: str, mx: torch.Tensor, rows: int, K: int, row_idx: Option
 def plan_linear_mx4(M: int, N: int, K: int):
     """(rows, columns) of op_linear_mx4's tiles, slices of the contraction, whether it takes the tile kernels; no GPU needed."""
     cols, slices, whole = C.c_int32(), C.c_int32(), C.c_int32()
-    rows = lib().dllmc_plan_linear_mx4(M, N, K, C.byref(cols), C.byref(slices), C.byref(whole))
+    fits = all(0 < v < 1 << 31 for v in (M, N, K))  # (of 32 bits)
+    rows = lib().dllmc_plan_linear_mx4(M, N, K, C.byref(cols), C.byref(slices), C.byref(whole)) if fits else 0
     if rows < 1:
         raise DllmcError("dllmc_plan_linear_mx4: invalid argument")
     return (rows, cols.value), slices.value, bool(whole.value)
@@ -925,7 +926,7 @@ def op_logprobs(dtype: str, logits: torch.Tensor, tokens: Optional[torch.Tensor]
     if not 0 <= top_k < 1 << 31 or M >= 1 << 31:
         raise DllmcError(f"op_logprobs: no {top_k} tokens of {M} rows")  # (what is allocated goes by them, and the call takes 32 bits)
     n = 0 if tokens is None else tokens.shape[-1]
-    tp = _need("tokens", tokens, torch.int32, (M, n), dev)
+    tp = _need("tokens", tokens, torch.int32, (M, n), dev) if n else None
     entropy = logits.new_empty(M, dtype=torch.float32)
     logp = None if tokens is None else logits.new_empty((M, n), dtype=torch.float32)
     ids = top = None
@@ -934,7 +935,7 @@ def op_logprobs(dtype: str, logits: torch.Tensor, tokens: Optional[torch.Tensor]
         ids = torch.empty_like(top, dtype=torch.int32)
     nbytes = _scratch_bytes("logprobs", code, M, vocab, top_k)
     scratch = _scratch(nbytes, logits)
-    _check(lib().dllmc_op_logprobs(code, logits.data_ptr(), ld, M, vocab, tp, n, top_k, _ptr(logp), entropy.data_ptr(), _ptr(ids),
+    _check(lib().dllmc_op_logprobs(code, logits.data_ptr(), ld, M, vocab, tp, n, top_k, _ptr(logp) if n else None, entropy.data_ptr(), _ptr(ids),
                                    _ptr(top), _ptr(scratch), nbytes, _stream(dev)), "dllmc_op_logprobs")
     return logp, entropy, ids, top
 
