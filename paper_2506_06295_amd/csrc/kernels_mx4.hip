@@ -17,21 +17,21 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // ---- rows in and out --------------------------------------------------------------------------------------
 // A workgroup per row; four lanes take a block.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_store(const T* __restrict__ x, int x_rows, const int* __restrict__ rows, int K, Mx4Tensor out) {
   const int i = blockIdx.x;
   const int row = rows ? rows[i] : i, len = static_cast<unsigned>(row) < static_cast<unsigned>(x_rows) ? K : 0;  // (no row: zeros)
   const T* r = x + static_cast<size_t>(len ? row : 0) * K;
   for (int t = threadIdx.x * 8; t < out.Kp; t += 2048) {
     float v[8];
-    load8<VEC>(r, t, len, v);
+    load8(r, t, len, v);
     const uint32_t scale = kv4_scale_byte(block32_top(v));
     *reinterpret_cast<uint32_t*>(out.codes + static_cast<size_t>(i) * (out.Kp / 2) + t / 2) = mx4_codes(v, scale);
     if (t % 32 == 0) out.scales[mx4_scale_at(i, t, out.Kp)] = static_cast<uint8_t>(scale);
   }
 }
 
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_load(Mx4Tensor in, const int* __restrict__ rows, int K, T* __restrict__ out) {
   const int i = blockIdx.x, r = rows ? rows[i] : i;
   const bool ok = static_cast<unsigned>(r) < static_cast<unsigned>(in.rows);
@@ -48,12 +48,12 @@ __global__ __launch_bounds__(256) void k_mx4_load(Mx4Tensor in, const int* __res
         v[2 * h + 1] = __uint_as_float(f[h] & 0xffff0000u);
       }
     }
-    store8<VEC>(o, t, K, v);
+    store8(o, t, K, v);
   }
 }
 
 // 8-bit rows back: q * scale, rounded to T
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, const float* __restrict__ scale, int q_rows, int K, int Kp,
                                                const int* __restrict__ rows, T* __restrict__ out) {
   const int i = blockIdx.x, r = rows ? rows[i] : i;
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void k_load8(const int8_t* __restrict__ q, con
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(static_cast<int8_t>((e < 4 ? w.x : w.y) >> (e % 4 * 8))) * s;
-    store8<VEC>(o, t, K, v);
+    store8(o, t, K, v);
   }
 }
 
@@ -526,37 +526,22 @@ __global__ __launch_bounds__(256, 1) void k_mx4_wide(Mx4Tensor a, Mx4Tensor w, T
   mx4_wide_body<T, MI, NJ>(a, w, out);
 }
 
-inline bool whole_pieces(const void* p, int K) { return K % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
 }  // namespace
 
-#define DLLMC_BY_TYPE(dtype, vec, CALL)      \
-  do {                                       \
-    if ((dtype) == 1 && (vec)) CALL(bf16_t, true);   \
-    else if ((dtype) == 1) CALL(bf16_t, false);      \
-    else if (vec) CALL(float, true);                 \
-    else CALL(float, false);                         \
-  } while (0)
-
 void launch_quant_mx4(int dtype, const void* x, int x_rows, const int* rows, int M, int K, Mx4Tensor out, hipStream_t st) {
-#define DLLMC_CALL(T, V) \
-  hipLaunchKernelGGL((k_mx4_store<T, V>), dim3(M), dim3(256), 0, st, static_cast<const T*>(x), x_rows, rows, K, out)
-  DLLMC_BY_TYPE(dtype, whole_pieces(x, K), DLLMC_CALL);
-#undef DLLMC_CALL
+  if (dtype == 1) hipLaunchKernelGGL(k_mx4_store<bf16_t>, dim3(M), dim3(256), 0, st, static_cast<const bf16_t*>(x), x_rows, rows, K, out);
+  else hipLaunchKernelGGL(k_mx4_store<float>, dim3(M), dim3(256), 0, st, static_cast<const float*>(x), x_rows, rows, K, out);
 }
 
 void launch_mx4_load(int dtype, Mx4Tensor in, const int* rows, int M, int K, void* out, hipStream_t st) {
-#define DLLMC_CALL(T, V) hipLaunchKernelGGL((k_mx4_load<T, V>), dim3(M), dim3(256), 0, st, in, rows, K, static_cast<T*>(out))
-  DLLMC_BY_TYPE(dtype, whole_pieces(out, K), DLLMC_CALL);
-#undef DLLMC_CALL
+  if (dtype == 1) hipLaunchKernelGGL(k_mx4_load<bf16_t>, dim3(M), dim3(256), 0, st, in, rows, K, static_cast<bf16_t*>(out));
+  else hipLaunchKernelGGL(k_mx4_load<float>, dim3(M), dim3(256), 0, st, in, rows, K, static_cast<float*>(out));
 }
 
 void launch_load8(int dtype, const int8_t* q, const float* scale, int q_rows, int K, const int* rows, int M, void* out, hipStream_t st) {
   const int Kp = static_cast<int>(i8_row_bytes(K));
-#define DLLMC_CALL(T, V) \
-  hipLaunchKernelGGL((k_load8<T, V>), dim3(M), dim3(256), 0, st, q, scale, q_rows, K, Kp, rows, static_cast<T*>(out))
-  DLLMC_BY_TYPE(dtype, whole_pieces(out, K), DLLMC_CALL);
-#undef DLLMC_CALL
+  if (dtype == 1) hipLaunchKernelGGL(k_load8<bf16_t>, dim3(M), dim3(256), 0, st, q, scale, q_rows, K, Kp, rows, static_cast<bf16_t*>(out));
+  else hipLaunchKernelGGL(k_load8<float>, dim3(M), dim3(256), 0, st, q, scale, q_rows, K, Kp, rows, static_cast<float*>(out));
 }
 
 namespace {

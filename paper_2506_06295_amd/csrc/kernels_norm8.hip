@@ -19,6 +19,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 }
 template <int NW> __device__ __forceinline__ double block_sum64(double v, double* red) {
   v = wave_sum64(v);
+  if (NW == 1) return v;
   if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
   __syncthreads();
   v = red[0];
@@ -27,12 +28,16 @@ template <int NW> __device__ __forceinline__ double block_sum64(double v, double
   return v;
 }
 
-// eight elements as 8-bit integers
+// Eight elements as 8-bit integers: a float32 number of at most 127 and 1.5 * 2^23 add up to the integer nearest to it, ties to even, in the low byte.
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float f) {
-  uint32_t w[2] = {0, 0};
+#pragma clang fp contract(off)  // (the product is a float32 number before it is rounded to an integer)
+  uint32_t b[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e / 4] |= (static_cast<uint32_t>(static_cast<int>(rintf(v[e] * f))) & 255u) << (e % 4 * 8);
-  return make_uint2(w[0], w[1]);
+  for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(v[e] * f + 12582912.f);
+  auto four = [](uint32_t a, uint32_t c, uint32_t d, uint32_t e) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(e, d, 0x0c0c0400u), __builtin_amdgcn_perm(c, a, 0x0c0c0400u), 0x05040100u);
+  };
+  return make_uint2(four(b[0], b[1], b[2], b[3]), four(b[4], b[5], b[6], b[7]));
 }
 __device__ __forceinline__ uint32_t top_of(const float (&v)[8], uint32_t top) {
 #pragma unroll
@@ -45,13 +50,13 @@ __device__ __forceinline__ void store_mx4(const float (&v)[8], int i, int t, con
   if (t % 32 == 0) mx.scales[mx4_scale_at(i, t, mx.Kp)] = static_cast<uint8_t>(byte);
 }
 
-// A workgroup per row.  PC > 0: the row, at most 2048 PC wide, stays in registers, PC pieces of eight elements a thread, and the gain is
-// requested with it: one trip to memory.  PC = 0, wider ones: its elements are read again for the norm, from the sum where it is kept (the thread's
+// A workgroup of TR threads per row.  PC > 0: the row, at most 8 TR PC wide, stays in registers, PC pieces of eight elements a thread, and the
+// gain is requested with it: one trip to memory.  PC = 0, wider ones: its elements are read again for the norm, from the sum where it is kept (the thread's
 // own writes: the sum may have taken the stream's place).
-template <typename T, typename S, bool I8, bool VEC, int PC>
-__global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restrict__ q, float* __restrict__ scale, Mx4Tensor mx) {
-  __shared__ double red[4];
-  __shared__ uint32_t redu[4];
+template <typename T, typename S, bool I8, bool WHOLE, int TR, int PC>
+__global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict__ q, float* __restrict__ scale, Mx4Tensor mx) {
+  __shared__ double red[TR / 64];
+  __shared__ uint32_t redu[TR / 64];
   const int i = blockIdx.x, d = n.d;
   const int row = n.rows ? n.rows[i] : i;
   const int len = static_cast<unsigned>(row) < static_cast<unsigned>(n.stream_rows) ? d : 0;  // (no row: zeros, and no sum)
@@ -62,7 +67,15 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restric
   const int Kp = I8 ? (d + 127) / 128 * 128 : mx.Kp;
   auto add = [&](float (&v)[8], const float (&y)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = roundf_to<S>(v[e] + y[e]);
+    for (int e = 0; e < 8; e += 2) {
+      v[e] += y[e];
+      v[e + 1] += y[e + 1];
+      if (sizeof(S) == 2) {
+        const uint32_t w = pack_bf16x2(v[e], v[e + 1]);
+        v[e] = __uint_as_float(w << 16);
+        v[e + 1] = __uint_as_float(w & 0xffff0000u);
+      }
+    }
   };
   double ss = 0.0;
   auto squares = [&](const float (&v)[8]) {
@@ -70,23 +83,23 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restric
     for (int e = 0; e < 8; ++e) ss += static_cast<double>(v[e]) * v[e];
   };
   auto root = [&] {  // (an infinity or NaN makes the whole row NaN, in either form)
-    ss = block_sum64<4>(ss, red);
+    ss = block_sum64<TR / 64>(ss, red);
     return ss < INFINITY ? static_cast<float>(1.0 / sqrt(ss / d + static_cast<double>(n.eps))) : NAN;
   };
   if constexpr (PC > 0) {
     float v[PC][8], y[PC][8], g[PC][8];
 #pragma unroll
-    for (int p = 0; p < PC; ++p) load8<VEC>(s, (p * 256 + threadIdx.x) * 8, len, v[p]);
+    for (int p = 0; p < PC; ++p) load8<WHOLE>(s, (p * TR + threadIdx.x) * 8, len, v[p]);
     if (x) {
 #pragma unroll
-      for (int p = 0; p < PC; ++p) load8<VEC>(x, (p * 256 + threadIdx.x) * 8, len, y[p]);
+      for (int p = 0; p < PC; ++p) load8<WHOLE>(x, (p * TR + threadIdx.x) * 8, len, y[p]);
     }
 #pragma unroll
-    for (int p = 0; p < PC; ++p) load8<VEC>(gain, (p * 256 + threadIdx.x) * 8, len, g[p]);
+    for (int p = 0; p < PC; ++p) load8<WHOLE>(gain, (p * TR + threadIdx.x) * 8, len, g[p]);
 #pragma unroll
     for (int p = 0; p < PC; ++p) {
       if (x) add(v[p], y[p]);
-      if (sum) store8<VEC>(sum, (p * 256 + threadIdx.x) * 8, len, v[p]);
+      if (sum) store8<WHOLE>(sum, (p * TR + threadIdx.x) * 8, len, v[p]);
       squares(v[p]);
     }
     const float rstd = root();
@@ -98,17 +111,17 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restric
       uint32_t top = 0;
 #pragma unroll
       for (int p = 0; p < PC; ++p) top = top_of(v[p], top);
-      const RowScale rs = row_scale(len ? block_max<4>(top, redu) : 0);
+      const RowScale rs = row_scale(len ? block_max<TR / 64>(top, redu) : 0);
       if (threadIdx.x == 0) scale[i] = rs.scale;
 #pragma unroll
       for (int p = 0; p < PC; ++p) {
-        const int t = (p * 256 + threadIdx.x) * 8;
+        const int t = (p * TR + threadIdx.x) * 8;
         if (t < Kp) *reinterpret_cast<uint2*>(q + static_cast<size_t>(i) * Kp + t) = rs.finite ? codes8(v[p], rs.f) : make_uint2(0, 0);
       }
     } else {
 #pragma unroll
       for (int p = 0; p < PC; ++p) {
-        const int t = (p * 256 + threadIdx.x) * 8;
+        const int t = (p * TR + threadIdx.x) * 8;
         if (t + 7 >= len) {  // (behind the row, where zero times a NaN or an infinity may stand)
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[p][e] = t + e < len ? v[p][e] : 0.f;
@@ -118,44 +131,44 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restric
     }
   } else {
     auto total = [&](int t, float (&v)[8]) {
-      load8<VEC>(s, t, len, v);
+      load8<WHOLE>(s, t, len, v);
       if (x) {
         float y[8];
-        load8<VEC>(x, t, len, y);
+        load8<WHOLE>(x, t, len, y);
         add(v, y);
       }
     };
-    for (int t = threadIdx.x * 8; t < len; t += 2048) {
+    for (int t = threadIdx.x * 8; t < len; t += 8 * TR) {
       float v[8];
       total(t, v);
-      if (sum) store8<VEC>(sum, t, len, v);
+      if (sum) store8<WHOLE>(sum, t, len, v);
       squares(v);
     }
     const float rstd = root();
     auto normed = [&](int t, float (&v)[8]) {
       float g[8];
-      if (sum) load8<VEC>(sum, t, len, v);
+      if (sum) load8<WHOLE>(sum, t, len, v);
       else total(t, v);
-      load8<VEC>(gain, t, len, g);
+      load8<WHOLE>(gain, t, len, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = t + e < len ? v[e] * rstd * g[e] : 0.f;
     };
     if constexpr (I8) {
       uint32_t top = 0;
-      for (int t = threadIdx.x * 8; t < len; t += 2048) {
+      for (int t = threadIdx.x * 8; t < len; t += 8 * TR) {
         float v[8];
         normed(t, v);
         top = top_of(v, top);
       }
-      const RowScale rs = row_scale(block_max<4>(top, redu));
+      const RowScale rs = row_scale(block_max<TR / 64>(top, redu));
       if (threadIdx.x == 0) scale[i] = rs.scale;
-      for (int t = threadIdx.x * 8; t < Kp; t += 2048) {
+      for (int t = threadIdx.x * 8; t < Kp; t += 8 * TR) {
         float v[8];
         normed(t, v);
         *reinterpret_cast<uint2*>(q + static_cast<size_t>(i) * Kp + t) = rs.finite ? codes8(v, rs.f) : make_uint2(0, 0);
       }
     } else {
-      for (int t = threadIdx.x * 8; t < Kp; t += 2048) {
+      for (int t = threadIdx.x * 8; t < Kp; t += 8 * TR) {
         float v[8];
         normed(t, v);
         store_mx4(v, i, t, mx);
@@ -164,23 +177,28 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormRows n, int8_t* __restric
   }
 }
 
+// Threads of a row and pieces of a thread by width.  Rows of up to 1024 go to a wavefront each, which waits for nobody (12288 x 256: 10.7 us, 23 with a
+// workgroup of four per row).  2049 to 4096 wide, us for 12288 rows of 4096; 3584; 4049: a bf16 stream 70.7; 57.8; 85 with 256 threads of two pieces and
+// 68.3; 62.5; 95 with 512 of one; a float32 one 105; 97; 116 and 100; 87; 119.  Bytes at a large copy's 5.8 TB/s: 61 and 95 (4096 wide).
 template <bool I8>
 void launch(int dtype, int stream_dtype, const NormRows& n, int8_t* q, float* scale, Mx4Tensor mx, hipStream_t st) {
-  const uintptr_t low = reinterpret_cast<uintptr_t>(n.x) | reinterpret_cast<uintptr_t>(n.stream) | reinterpret_cast<uintptr_t>(n.gain) |
-                        reinterpret_cast<uintptr_t>(n.sum_out);
-  const bool vec = n.d % 8 == 0 && low % 16 == 0;
-#define DLLMC_N(T, S, V, PC) hipLaunchKernelGGL((k_norm_rows<T, S, I8, V, PC>), dim3(n.M), dim3(256), 0, st, n, q, scale, mx)
-#define DLLMC_NV(T, S) \
-  if (!vec && n.d <= 4096) DLLMC_N(T, S, false, 2); \
-  else if (!vec) DLLMC_N(T, S, false, 0); \
-  else if (n.d <= 2048) DLLMC_N(T, S, true, 1); \
-  else if (n.d <= 4096) DLLMC_N(T, S, true, 2); \
-  else if (n.d <= 8192) DLLMC_N(T, S, true, 4); \
-  else DLLMC_N(T, S, true, 0)
-  if (dtype == 0) { DLLMC_NV(float, float); }
-  else if (stream_dtype == 0) { DLLMC_NV(bf16_t, float); }
-  else { DLLMC_NV(bf16_t, bf16_t); }
-#undef DLLMC_NV
+#define DLLMC_N(T, S, TR, PC)                                                                                                     \
+  do {                                                                                                                          \
+    if (n.d % 8 == 0) hipLaunchKernelGGL((k_norm_rows<T, S, I8, true, TR, PC>), dim3(n.M), dim3(TR), 0, st, n, q, scale, mx);     \
+    else hipLaunchKernelGGL((k_norm_rows<T, S, I8, false, TR, PC>), dim3(n.M), dim3(TR), 0, st, n, q, scale, mx);                 \
+  } while (0)
+#define DLLMC_BY_WIDTH(T, S)               \
+  if (n.d <= 512) DLLMC_N(T, S, 64, 1);        \
+  else if (n.d <= 1024) DLLMC_N(T, S, 64, 2);  \
+  else if (n.d <= 2048) DLLMC_N(T, S, 256, 1); \
+  else if (n.d <= 4096) DLLMC_N(T, S, (sizeof(S) == 4 ? 512 : 256), (sizeof(S) == 4 ? 1 : 2)); \
+  else if (n.d <= 8192) DLLMC_N(T, S, 512, 2); \
+  else if (n.d <= 12288) DLLMC_N(T, S, 512, 3); \
+  else DLLMC_N(T, S, 512, 0)
+  if (dtype == 0) { DLLMC_BY_WIDTH(float, float); }
+  else if (stream_dtype == 0) { DLLMC_BY_WIDTH(bf16_t, float); }
+  else { DLLMC_BY_WIDTH(bf16_t, bf16_t); }
+#undef DLLMC_BY_WIDTH
 #undef DLLMC_N
 }
 

@@ -47,31 +47,43 @@ __device__ __forceinline__ uint32_t block32_top(const float (&v)[8]) {
   return max(top, __float_as_uint(dpp_xor2(__uint_as_float(top))));
 }
 
-// Elements t .. t + 7 of a row of `len`, zeros behind it.  VEC: the row is 16-byte aligned and len a multiple of 8.
-template <bool VEC, typename T> __device__ __forceinline__ void load8(const T* row, int t, int len, float (&v)[8]) {
-  if (VEC) {
-    if (t < len) {
-      Eight<T>::load(row + t, v);
-    } else {
+// Elements t .. t + 7 of a row of `len`, zeros behind it.  Rows start at any element: the vector memory instructions take 16 bytes at any address
+// that is a multiple of the element's size.  WHOLE: len is a multiple of 8.
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+template <bool WHOLE = false> __device__ __forceinline__ void load8(const bf16_t* row, int t, int len, float (&v)[8]) {
+  if (t + 8 <= len) {
+    const u32x4_at2 a = *reinterpret_cast<const u32x4_at2*>(row + t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    }
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e % 2 ? a[e / 2] & 0xffff0000u : a[e / 2] << 16);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = t + e < len ? ldf(row + t + e) : 0.f;
+    for (int e = 0; e < 8; ++e) v[e] = !WHOLE && t + e < len ? ldf(row + t + e) : 0.f;
   }
 }
-template <bool VEC, typename T> __device__ __forceinline__ void store8(T* row, int t, int len, const float (&v)[8]) {
-  if (VEC) {
-    if (t >= len) return;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(row + t) =
-          make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-    } else {
-      reinterpret_cast<float4*>(row + t)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(row + t)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    }
+template <bool WHOLE = false> __device__ __forceinline__ void load8(const float* row, int t, int len, float (&v)[8]) {
+  if (t + 8 <= len) {
+    const u32x4_at4 a = *reinterpret_cast<const u32x4_at4*>(row + t), b = *reinterpret_cast<const u32x4_at4*>(row + t + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? a[e % 4] : b[e % 4]);
   } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = !WHOLE && t + e < len ? ldf(row + t + e) : 0.f;
+  }
+}
+__device__ __forceinline__ void store_pieces(bf16_t* p, const float (&v)[8]) {
+  *reinterpret_cast<u32x4_at2*>(p) = u32x4_at2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store_pieces(float* p, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 8; h += 4)
+    *reinterpret_cast<u32x4_at4*>(p + h) =
+        u32x4_at4{__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])};
+}
+template <bool WHOLE = false, typename T> __device__ __forceinline__ void store8(T* row, int t, int len, const float (&v)[8]) {
+  if (t + 8 <= len) {
+    store_pieces(row + t, v);
+  } else if (!WHOLE) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (t + e < len) stf(row + t + e, v[e]);
