@@ -487,7 +487,7 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
 /* ---- from the residual stream to token log probabilities, in few bits -----------------------
  * A sublayer's output added to the stream and its norm as rows for the maps in few bits; linear maps on 4-bit blocks, whose weights
  * are half the bytes of 8-bit ones; and what the logits say about tokens beyond the greedy one.  Memory, scratch, captures and
- * alignment as above, where nothing else is said; M < 2^24.
+ * alignment as above, where nothing else is said; M < 2^24, of the norms and the log probabilities M < 2^23.
  *
  * s = stream[r] + x[i] (stream[r] if x is NULL), rounded to stream_dtype, r = row_idx[i] (i if NULL);
  * h = (s * rstd) * gain in float32, rstd = 1 / sqrt(mean of s^2 + eps) rounded to float32 from 64 bits.  Row i of the result: h
@@ -524,7 +524,7 @@ size_t dllmc_op_linear_mx4_scratch_bytes(int32_t M, int32_t N, int32_t K);
 int dllmc_op_linear_mx4(int32_t dtype, const void* a, int32_t M, const void* w, int32_t N, int32_t K, void* out, void* scratch,
                         size_t scratch_bytes, void* hip_stream);
 
-/* Of every row of logits [M, vocab] (dtype; row i at i * ld elements, ld >= vocab; M < 2^23, vocab <= 2^24, M * vocab <= 2^40): the log probabilities under its softmax
+/* Of every row of logits [M, vocab] (dtype; row i at i * ld elements, ld >= vocab; vocab <= 2^24, M * vocab <= 2^40): the log probabilities under its softmax
  * of n_given <= 65536 given tokens (logp [M, n_given] for tokens [M, n_given]; minus infinity for an id outside [0, vocab)), its entropy [M],
  * and the top_k <= 64 likeliest tokens, most likely first, of equal logits the lower id first (top_ids, top_logp [M, top_k]).  tokens and
  * logp are NULL and n_given 0, top_ids and top_logp NULL and top_k 0, entropy NULL, where that is not asked for.  A logit of minus infinity

@@ -1459,7 +1459,8 @@ bool logits_ok(int32_t M, int32_t vocab) {
 bool norm_ok(int32_t dtype, int32_t stream_dtype, const void* x, const void* stream, int32_t stream_rows, const int32_t* row_idx,
              int32_t M, int32_t d, const void* gain, float eps, const void* sum_out, const Bytes& out, const Bytes& out2) {
   if (!dtype_ok(dtype) || !dtype_ok(stream_dtype) || (dtype == DLLMC_F32 && stream_dtype != DLLMC_F32)) return false;
-  if (!stream || !gain || !out.p || M < 1 || M >= kMaxRows || d < 1 || d > kMaxI8K || stream_rows < 1) return false;
+  // (a row takes up to 512 work-items of a launch's 2^32)
+  if (!stream || !gain || !out.p || M < 1 || M >= kMaxRows / 2 || d < 1 || d > kMaxI8K || stream_rows < 1) return false;
   if (row_idx == nullptr && M > stream_rows) return false;
   if (!(eps >= 0.f) || !(eps < INFINITY)) return false;
   const size_t esz = elem_bytes(dtype), ssz = elem_bytes(stream_dtype);

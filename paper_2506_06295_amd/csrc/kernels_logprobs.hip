@@ -372,7 +372,7 @@ __global__ __launch_bounds__(256) void k_logprobs_short(LogprobRows r) {
     }
     if (lane < r.top_k) best[lane] = 0;
     if (count <= kShortFound) {
-      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       for (int a = lane; a < count; a += 64) {
         const u64 own = found[a];
         int rank = 0;
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256) void k_logprobs_short(LogprobRows r) {
         last = next;
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   finish_row<64>(r, i, row.l, t, best);
 }

@@ -77,17 +77,17 @@ __device__ __forceinline__ i32x8 operand(const i32x4& u) { return i32x8{u[0], u[
 
 typedef const __attribute__((address_space(1))) int* global_int_ptr;  // (a pointer put together from registers: a flat load otherwise)
 
-// four neighbouring results of a row, n0 + 4 <= N or element by element
+// four neighbouring results of a row at any address, those before column N
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int n, int N, bool whole, float a, float b, float c, float d) {
-  if (whole) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
-    else *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+__device__ __forceinline__ void store4(T* p, int n, int N, float a, float b, float c, float d) {
+  if (n + 4 <= N) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_at2*>(p) = u32x2_at2{pack_bf16x2(a, b), pack_bf16x2(c, d)};
+    else *reinterpret_cast<u32x4_at4*>(p) = u32x4_at4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
   } else {
     if (n < N) stf(p, a);
     if (n + 1 < N) stf(p + 1, b);
     if (n + 2 < N) stf(p + 2, c);
-    if (n + 3 < N) stf(p + 3, d);
   }
 }
 
@@ -233,9 +233,8 @@ __device__ __forceinline__ void mx4_ring_body(const Mx4Tensor& a, const Mx4Tenso
     const int j = x % NB, rb = x / NB;
     const int m = m0 + rb * 16 + ln, n = n0 + j * 16 + lg * 4;
     if (m >= M || n >= N) continue;
-    const bool whole = n + 4 <= N && N % 4 == 0;
-    if (gridDim.z == 1) store4(out + static_cast<size_t>(m) * N + n, n, N, whole, sum[0], sum[1], sum[2], sum[3]);
-    else store4(sums + (static_cast<size_t>(blockIdx.z) * M + m) * N + n, n, N, whole, sum[0], sum[1], sum[2], sum[3]);
+    if (gridDim.z == 1) store4(out + static_cast<size_t>(m) * N + n, n, N, sum[0], sum[1], sum[2], sum[3]);
+    else store4(sums + (static_cast<size_t>(blockIdx.z) * M + m) * N + n, n, N, sum[0], sum[1], sum[2], sum[3]);
   }
 }
 
@@ -483,41 +482,41 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
   constexpr int kPer = 16 / sizeof(T), kRow = NJ * 32 / kPer;  // elements and slots of 16 bytes
   constexpr int kPitch = kRow + 1;
   static_assert(4 * 32 * kPitch <= DA * kSlotA + DB * kSlotB, "results fit the ring");
-  if (N % kPer == 0) {  // (kernel-uniform)
-    __syncthreads();
-    uint4* mine = lds + wave * 32 * kPitch;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          store4(reinterpret_cast<T*>(mine + ln * kPitch) + j * 32 + q * 8 + lg * 4, 0, 4, true, acc[i][j][4 * q], acc[i][j][4 * q + 1],
-                 acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int s = 0; s < 32 * kRow / 64; ++s) {
-        const int at = s * 64 + lane, r = at / kRow, c = at % kRow;
-        const int m = m0 + wm * (MI * 32) + i * 32 + r, n = n0 + wn * (NJ * 32) + c * kPer;
-        const i32x4 v = __builtin_bit_cast(i32x4, mine[r * kPitch + c]);
-        if (m < M && n < N) *reinterpret_cast<i32x4*>(out + static_cast<size_t>(m) * N + n) = v;
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-    return;
-  }
+  __syncthreads();
+  uint4* mine = lds + wave * 32 * kPitch;
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
-    const int m = m0 + wm * (MI * 32) + i * 32 + ln;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int n = n0 + wn * (NJ * 32) + j * 32 + q * 8 + lg * 4;
-        if (m < M && n < N)
-          store4(out + static_cast<size_t>(m) * N + n, n, N, N % 4 == 0, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
-                 acc[i][j][4 * q + 3]);
+        const f32x16& v = acc[i][j];
+        T* to = reinterpret_cast<T*>(mine + ln * kPitch) + j * 32 + q * 8 + lg * 4;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[4 * q], v[4 * q + 1]), pack_bf16x2(v[4 * q + 2], v[4 * q + 3]));
+        else *reinterpret_cast<float4*>(to) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
       }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int s = 0; s < 32 * kRow / 64; ++s) {
+      const int at = s * 64 + lane, r = at / kRow, c = at % kRow;
+      const int m = m0 + wm * (MI * 32) + i * 32 + r, n = n0 + wn * (NJ * 32) + c * kPer;
+      const i32x4 v = __builtin_bit_cast(i32x4, mine[r * kPitch + c]);
+      T* to = out + static_cast<size_t>(m) * N + n;
+      if (m >= M) continue;
+      if (n + kPer <= N) {
+        *reinterpret_cast<typename std::conditional<sizeof(T) == 2, u32x4_at2, u32x4_at4>::type*>(to) = __builtin_bit_cast(u32x4_at4, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          if (n + e < N) {
+            const uint32_t w = static_cast<uint32_t>(v[e * sizeof(T) / 4]);
+            if constexpr (sizeof(T) == 2) to[e] = static_cast<bf16_t>(e % 2 ? w >> 16 : w);
+            else to[e] = __uint_as_float(w);
+          }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);  // (no addresses of later rows beside the accumulators)
   }
 }
 

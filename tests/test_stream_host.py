@@ -52,7 +52,7 @@ CALLS = {"dllmc_op_norm_quant8": NORM8, "dllmc_op_norm_mx4": NORM4, "dllmc_op_lo
          "dllmc_op_mx4_load": LOAD4, "dllmc_op_linear_mx4": LINEAR, "dllmc_op_logprobs": LOGPROBS}
 
 BAD_NORM = [dict(dtype=2), dict(dtype=F32, stream_dtype=BF16), dict(stream_dtype=2), dict(stream=None), dict(gain=None), dict(M=0), dict(M=-1),
-            dict(M=1 << 24), dict(d=0), dict(d=131073), dict(rows=0), dict(row_idx=None, M=10), dict(eps=f(-1e-6)), dict(eps=f(INF)),
+            dict(M=1 << 23), dict(M=1 << 24), dict(d=0), dict(d=131073), dict(rows=0), dict(row_idx=None, M=10), dict(eps=f(-1e-6)), dict(eps=f(INF)),
             dict(eps=f(float("nan"))), dict(x=near(p(0), 1)), dict(stream=near(p(1), 2)), dict(gain=near(p(3), 1)), dict(row_idx=near(p(2), 2)),
             dict(sum_out=near(p(4), 2)),
             dict(sum_out=p(1)),                                  # the stream's place, but rows are listed
