@@ -290,22 +290,24 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
   xcd_tile_map_blocked(col_tile, row_tile);
   const int m0 = row_tile * BM, n0 = col_tile * BN;
 
+  // Chunk c of a tile's row r lies in slot c ^ turn(r): rows 0 .. 7 and 16 .. 23 of 32, whose reads share a cycle, meet in no bank (4 cycles a read; with
+  // r % 8 in its place 8, counted).
+  auto turn = [](int r) { return (r >> 1 & 3) | (r >> 2 & 4); };
   // loader: wavefront v issues instructions L v .. L v + L - 1 of an operand, 8 rows each: a scalar base and a lane offset
   // (rows past the last one: the last one; groups of scales likewise)
   const char *abase[LA], *bbase[LB], *asbase[MI], *bsbase[NJ];
   uint32_t aoff[LA], boff[LB];
-  const int chunk = ((lane % 8) ^ (lane / 8)) * 16;
 #pragma unroll
   for (int j = 0; j < LA; ++j) {
     const int r = min(m0 + 8 * (LA * wave + j), M - 1);
     abase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(a.codes + static_cast<size_t>(r) * row_bytes));
-    aoff[j] = static_cast<uint32_t>(min(lane / 8, M - 1 - r) * row_bytes + chunk);
+    aoff[j] = static_cast<uint32_t>(min(lane / 8, M - 1 - r) * row_bytes + (lane % 8 ^ turn(8 * (LA * wave + j) + lane / 8)) * 16);
   }
 #pragma unroll
   for (int j = 0; j < LB; ++j) {
     const int r = min(n0 + 8 * (LB * wave + j), N - 1);
     bbase[j] = wave_uniform_ptr(reinterpret_cast<const char*>(w.codes + static_cast<size_t>(r) * row_bytes));
-    boff[j] = static_cast<uint32_t>(min(lane / 8, N - 1 - r) * row_bytes + chunk);
+    boff[j] = static_cast<uint32_t>(min(lane / 8, N - 1 - r) * row_bytes + (lane % 8 ^ turn(8 * (LB * wave + j) + lane / 8)) * 16);
   }
   // scales: in LDS one load of four groups a wavefront, else one of a group for each of its blocks
   const int group = min(wave * 4 + lane / 16, (BM + BN) / 32 - 1);
@@ -393,10 +395,10 @@ __device__ __forceinline__ void mx4_wide_body(const Mx4Tensor& a, const Mx4Tenso
     const int s = q / (MI + NJ), x = q % (MI + NJ), c = (half * 2 + s) * 2 + lg;
     if (x < NJ) {
       const int r = wn * (NJ * 32) + x * 32 + ln;
-      bf[half][s][x] = __builtin_bit_cast(i32x4, lds[DA * kSlotA + slot_b * kSlotB + r * 8 + (c ^ (r % 8))]);
+      bf[half][s][x] = __builtin_bit_cast(i32x4, lds[DA * kSlotA + slot_b * kSlotB + r * 8 + (c ^ turn(r))]);
     } else {
       const int r = wm * (MI * 32) + (x - NJ) * 32 + ln;
-      af[half][s][x - NJ] = __builtin_bit_cast(i32x4, lds[slot_a * kSlotA + r * 8 + (c ^ (r % 8))]);
+      af[half][s][x - NJ] = __builtin_bit_cast(i32x4, lds[slot_a * kSlotA + r * 8 + (c ^ turn(r))]);
     }
   };
   constexpr int kReads = 2 * (MI + NJ), kMfma = 2 * MI * NJ;
