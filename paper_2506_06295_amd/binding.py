@@ -833,7 +833,8 @@ def op_norm_quant8(dtype: str, stream: torch.Tensor, gain: torch.Tensor, eps: fl
                    sum_out: Optional[torch.Tensor] = None):
     """(int8 [M, i8_row_bytes(d)], float32 [M], sums [M, d]): the RMS norm of rows row_idx (int32 [M]; all if None) of stream [*, d]
     plus x [M, d] as op_quant8 holds rows, and those sums in the stream's type (None without x and sum_out).  stream_dtype: dtype if
-    None.  sum_out: where the sums go (may be stream, or x)."""
+    None.  sum_out: where the sums go (may be stream, or x).  Where row_idx names no row the result is zeros, and that row of the sums is not
+    written (a tensor made here holds anything there)."""
     args, op, sum_out, dev = _norm_operands(dtype, stream, gain, x, row_idx, stream_dtype, sum_out)
     M, d = args[6], args[7]
     q, scale = stream.new_empty((M, i8_row_bytes(d)), dtype=torch.int8), stream.new_empty(M, dtype=torch.float32)

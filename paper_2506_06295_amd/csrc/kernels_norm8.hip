@@ -182,7 +182,7 @@ __global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict
 
 // Threads of a row and pieces of a thread by width.  Rows of up to 1024 go to a wavefront each, which waits for nobody (12288 x 256: 10.7 us, 23 with a
 // workgroup of four per row).  2049 to 4096 wide, us for 12288 rows of 4096; 3584; 4049: a bf16 stream 70.7; 57.8; 85 with 256 threads of two pieces and
-// 68.3; 62.5; 95 with 512 of one; a float32 one 105; 97; 116 and 100; 87; 119.  Bytes at a large copy's 5.8 TB/s: 61 and 95 (4096 wide).
+// 68.3; 62.5; 95 with 512 of one; a float32 one 105; 97; 116 and 100; 87; 119.  The bytes of 4096 wide take 71 and 112 at 4.95 TB/s, a copy of 4 GB's.
 template <bool I8>
 void launch(int dtype, int stream_dtype, const NormRows& n, int8_t* q, float* scale, Mx4Tensor mx, hipStream_t st) {
 #define DLLMC_N(T, S, TR, PC)                                                                                                     \
