@@ -490,7 +490,8 @@ int dllmc_op_linear_i8(int32_t dtype, const int8_t* a, const float* a_scale, int
  * alignment as above, where nothing else is said; M < 2^24, of the norms and the log probabilities M < 2^23.
  *
  * s = stream[r] + x[i] (stream[r] if x is NULL), rounded to stream_dtype, r = row_idx[i] (i if NULL);
- * h = (s * rstd) * gain in float32, rstd = 1 / sqrt(mean of s^2 + eps) rounded to float32 from 64 bits.  Row i of the result: h
+ * h = (s * rstd) * gain in float32, rstd = 1 / sqrt(mean of s^2 + eps) rounded from 64 bits to float32's 24 (also where it lies outside
+ * float32's normal numbers: with eps = 0 every finite row that is not of zeros has its norm).  Row i of the result: h
  * as dllmc_op_quant8 (norm_quant8) or dllmc_op_quant_mx4 (norm_mx4) would hold it.  x [M, d] and gain [d] of dtype, stream
  * [stream_rows, d] of stream_dtype (dtype, or DLLMC_F32), all aligned to their elements; d <= 131072, 0 <= eps < infinity.  sum_out
  * [M, d] of stream_dtype (may be NULL): s; it may be the stream (row_idx NULL) or, of the same type, x.  An r outside

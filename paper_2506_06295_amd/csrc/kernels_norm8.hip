@@ -3,7 +3,8 @@
 //   s = stream[r] + x[i], rounded to the stream's type;  h = (s * rstd) * g, rstd = 1 / sqrt(mean s^2 + eps);  h in few bits.
 //
 // Squares are summed in 64 bits: every finite row has a norm (squares of float32 or bf16 numbers pass float32's range), and the order in which a
-// kernel adds them does not reach the codes.  Everything else is float32.
+// kernel adds them does not reach the codes.  Everything else is float32.  rstd can pass float32's range too (rows of subnormals
+// with eps = 0) and fall below its normal numbers (rows near its largest): then s takes a power of two first and rstd goes without it.
 //
 // Bound by the bytes with many rows: x, stream, sum and codes of 12288 rows of 4096 (bf16, 8 bits) in 70.7 us, 5.0 TB/s; by two trips to memory and a
 // launch with few: 64 rows 4.3 us.
@@ -85,9 +86,19 @@ __global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += static_cast<double>(v[e]) * v[e];
   };
-  auto root = [&] {  // (an infinity or NaN makes the whole row NaN, in either form)
+  // (An infinity or NaN makes the whole row NaN, in either form; zeros with eps = 0 do as well.)
+  auto root = [&] {
     ss = block_sum64<TR / 64>(ss, red);
-    return ss < INFINITY ? static_cast<float>(1.0 / sqrt(ss / d + static_cast<double>(n.eps))) : NAN;
+    return ss < INFINITY ? 1.0 / sqrt(ss / d + static_cast<double>(n.eps)) : static_cast<double>(NAN);
+  };
+  // h = ((s * pre) * (rstd / pre)) * g, the second factor a normal float32 number.  pre = 1 but at both ends, where a root mean square lies under 2^-126
+  // (rstd at most 2^157.5: one element of 2^-149 in 131072) or over 2^126 (rstd at least 2^-128).  What s * pre loses there is far
+  // below what the products keep.
+  auto inside = [](float rstd) { return rstd >= 0x1p-126f && rstd <= 0x1p126f; };
+  auto at_an_end = [](double r, float& rstd) {
+    const bool low = r < 1.0;
+    rstd = static_cast<float>(r * (low ? 0x1p4 : 0x1p-32));
+    return low ? 0x1p-4f : 0x1p32f;
   };
   if constexpr (PC > 0) {
     float v[PC][8], y[PC][8], g[PC][8];
@@ -105,7 +116,15 @@ __global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict
       if (sum) store8<WHOLE>(sum, (p * TR + threadIdx.x) * 8, len, v[p]);
       squares(v[p]);
     }
-    const float rstd = root();
+    const double r = root();
+    float rstd = static_cast<float>(r);
+    if (!inside(rstd)) {
+      const float pre = at_an_end(r, rstd);
+#pragma unroll
+      for (int p = 0; p < PC; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] *= pre;
+    }
 #pragma unroll
     for (int p = 0; p < PC; ++p)
 #pragma unroll
@@ -147,14 +166,16 @@ __global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict
       if (sum) store8<WHOLE>(sum, t, len, v);
       squares(v);
     }
-    const float rstd = root();
+    const double r = root();
+    float rstd = static_cast<float>(r);
+    const float pre = inside(rstd) ? 1.f : at_an_end(r, rstd);
     auto normed = [&](int t, float (&v)[8]) {
       float g[8];
       if (sum) load8<WHOLE>(sum, t, len, v);
       else total(t, v);
       load8<WHOLE>(gain, t, len, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = t + e < len ? v[e] * rstd * g[e] : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] = t + e < len ? v[e] * pre * rstd * g[e] : 0.f;
     };
     if constexpr (I8) {
       uint32_t top = 0;
