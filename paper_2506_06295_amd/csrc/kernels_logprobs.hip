@@ -7,15 +7,17 @@
 //
 // The likeliest tokens come from the same pass.  A block is the 32 logits that a thread takes at a time; their maximum is at hand and stays in LDS.
 // At the end the k-th largest of the threads' maxima bounds the k-th logit from below, the few blocks that reach it are read once more
-// (k of 32 logits: they are in a cache), and what reaches it there is ranked by counting.  Where that is too many logits (rows of
-// equal ones) the row is walked once per alternative.
+// (k of 32 logits: they are in a cache), and what reaches it there is ranked by counting.  Where that is too many logits the row is
+// walked once per alternative: rows of equal ones (1024 of 126464 in bf16, k = 8: 1420 us), float32 logits so far from zero that the bound's 16 bits
+// tell few of them apart (1024 x 126464, k = 8, deviation 2: 93 us about 0, 108 about 500, 2110 about 1000).
 //
 // k_logprobs takes a row, or where there are few rows a slice of one, with a workgroup; a second launch joins slices.  k_logprobs_short takes
 // rows of up to 2048 logits with a wavefront each.
 //
-// Bound by the bytes where there are many: 4096 rows of 152064 bf16 logits, the eight likeliest of each, 234 us (5.3 TB/s; a logit costs 9 vector
-// instructions and an exponential, 200 us of the card's), 1024 rows of 126464 in float32 91 (5.7).  Few rows are two dependent launches: 64 rows of
-// 126464 13.4 us, one row 10.7 (the second launch 4.5 of it).
+// Bound by the bytes where there are many: 4096 rows of 152064 bf16 logits, the eight likeliest of each, 229 us (5.4 TB/s; a logit costs 9 vector
+// instructions and an exponential, 200 us of the card's), 1024 rows of 126464 in float32 93 (5.6).  Few rows are two dependent launches: 64 rows of
+// 126464 15.8 us (13.3 with logits from the memory-side cache), one row 10.7 (the second launch 4.5 of it).  Times here: the best of several means of
+// launches behind one another.
 #include <cmath>
 #include <type_traits>
 
@@ -335,7 +337,9 @@ __global__ __launch_bounds__(256) void k_logprobs_join(LogprobRows r, int slices
 
 // ---- short rows -------------------------------------------------------------------------------------------
 // A wavefront per row of up to 2048 logits (with what lies before it in its first line), a lane's 32 in registers; no wavefront waits for another
-// (16384 x 1024 in bf16, k = 8: 21.5 us, 64 with a workgroup per row).
+// (16384 x 1024 in bf16, k = 8: 22.4 us, 64 with a workgroup per row).  The bound is the k-th of 64 lanes' maxima, a weak one for k near 64: some 43
+// logits reach it at k = 32 and 160 at 60; at 63 and 64 there are more than the list takes in one of six rows and in half of them, and those rows are
+// walked (the same rows, k = 0; 8; 32; 48; 60; 63; 64: 13.3; 22.4; 27.7; 37.8; 69; 191; 291 us; rows of equal logits, k = 8: 66).
 constexpr int kShort = 64 * kBlock, kShortFound = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void k_logprobs_short(LogprobRows r) {
@@ -408,8 +412,9 @@ __global__ __launch_bounds__(256) void k_logprobs_short(LogprobRows r) {
 
 struct Cut { int slices, per; };
 // Slices of whole chunks: four workgroups for every CU where there are fewer rows than CUs, one launch beyond, and no more chunks than the maxima's
-// room.  One slice and some 1024 workgroups, us: 256 rows of 126464 in float32 25.9 and 30.1, 500 rows 41.9 and 47.6, 1000 of 152064 in bf16 59 and 66
-// (but 300 of 126464 29.7 and 25.1); 200 rows 25.5 (two slices) and 26.4, in bf16 25.2 and 22.5; 64 rows 14.6 (four) and 13.3.
+// room.  One slice and some 1024 workgroups, us, logits of 126464 from memory: float32 64 rows 22.3 and 15.8, 128 27.3 and 21.2, 200 29.1 and 28.9, 256
+// 30.7 and 32.4, 500 50.8 and 54.0; bf16 128 rows 25.4 and 17.1, 256 32.7 and 23.7, 300 35.2 and 26.6, 500 37.1 and 36.2, 700 43.8 and 46.0.  The
+// limit is float32's: bf16 rows of half the bytes would do better with slices up to some 500 rows.
 Cut cut_rows(int dtype, int M, int vocab) {
   const int before = (dtype == 1 ? 64 : 32) - 1;  // (logits that a row's first line may hold before it)
   if (vocab + before <= kShort) return {0, 0};

@@ -3,6 +3,8 @@
 // A block is 32 neighbouring elements of a row: codes of 4 bits (sign, and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) times one power of two, as
 // in a 4-bit cache.  The scaled matrix instructions multiply codes exactly and take both blocks' powers of two along, so the only roundings of
 // out[i][j] = sum_k a[i][k] w[j][k] are those of float32 sums and of the result.
+//
+// Times here: the best of several means of 20 launches behind one another.
 #include <type_traits>
 
 #include "mx4.hpp"
@@ -97,8 +99,8 @@ __device__ __forceinline__ void store4(T* p, int n, int N, float a, float b, flo
 // from global memory straight into LDS through a ring of stages.  RG wavefronts take 16 RB rows each, 8 / RG share the
 // contraction: a stage is 64 * 8 / RG bytes of every row's codes, and a wavefront multiplies its own 64 of them, 128 elements, with one 16 x 16 x 128
 // product a block.  Their sums meet in LDS at the end, in one order.  Slice blockIdx.z of the contraction; with one slice results leave
-// rounded, else as float32 sums for k_mx4_sum.  One row of 12288 x 4096 takes 7.0 us, 16 rows the same, 64 rows 9.2; the weights' bytes are 5.4 at a
-// copy's rate, a launch alone some 2.
+// rounded, else as float32 sums for k_mx4_sum.  One row of 12288 x 4096 takes 7.5 us with weights from memory, 16 rows the same, 64 rows 10.1 (6.9, 7.0 and
+// 8.8 with weights from the memory-side cache); the weights' bytes are 5.4 at a copy's rate, a launch alone some 2.
 template <int RG, int RB, int NB> struct Mx4Ring {
   static constexpr int KW = 8 / RG, SS = KW / 2;  // wavefronts along the contraction, 128-byte lines of a stage
   static constexpr int BM = 16 * RG * RB, R = BM + 16 * NB;
@@ -262,9 +264,10 @@ __global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ sums,
 // are one more load of every wavefront (16 groups of 32 rows' 256 bytes, of rows first, then columns) and travel with the ring of X; the tile of
 // 256 x 256 fills LDS (two stages of each operand instead would leave Y half a step to land), and its wavefronts load their own blocks' scales
 // into registers, a step ahead.
-// What bounds it is the card's power: 12288 x 12288 x 4096 takes 289 us (4.3 PFLOP/s), of zeros 210; a step of random operands 1.56 us at 1.8 GHz (bare
-// products 1.24), of zeros 0.97 (0.88); MFMAs run in 72 % of the main loop's cycles.  The results take 40 us of it, the rate of a copy; delaying
-// half of the CUs, so that some store while others multiply, gave 2 %.
+// What bounds it is the card's power: 12288 x 12288 x 4096 takes 297 us (4.2 PFLOP/s), of zeros 206; a step of random operands 1.6 us at 1.8 GHz (bare
+// products 1.24), of zeros 1.0 (0.88).  MFMAs run in 60 % of the launch's cycles, in 73 % of those of a copy that ends with its main loop and takes
+// 260 us: the results cost 37, less than a fill of as many bytes alone (43); delaying half of the CUs, so that some store while others
+// multiply, gave 2 % at this size.
 template <int BM, int BN> struct Mx4Rings {
   static constexpr bool kInLds = BM + BN < 512;
   static constexpr int kRoom = kInLds ? 1280 - 4 * 32 : 1280;  // rows of 128 bytes, beside four stages of scales
@@ -553,10 +556,12 @@ void launch_load8(int dtype, const int8_t* q, const float* scale, int q_rows, in
 namespace {
 
 // Tile and slices with the lowest estimate, us: start + rounds of 256 workgroups x (round + line x 128-byte lines) + MB of weights x w + MB of
-// results x out, or of float32 sums x sums + the launch that adds them.  Fitted (4 to 9 % rms) to 2300 launches, cold weights, 1 to 12288 rows of
+// results x out, or of float32 sums x sums + the launch that adds them.  Fitted (4 to 9 % rms) to 2300 launches, weights from memory, 1 to 12288 rows of
 // thirteen maps of 256 to 126464 outputs; the choices are 1.6 % from the quickest on average.  The shapes are those of 24 without which they
-// would be further: 64 x 12288 x 4096 9.2 us (tiles of 128 x 64; 11.8 of 128 x 128), 1280 x 18944 x 3584 48.8 in two rounds of 256 x 192 (55.6 of
-// 256 x 256, 61.7 of 192 x 256, a third round for six tiles), 1 x 12288 x 4096 7.0 (16 x 48) and 11.1 (16 x 16, three rounds).
+// would be further: 64 x 12288 x 4096 10.4 us (64 x 64; 9.7 of 128 x 64, 12.0 of 128 x 128, 14.4 of 32 x 64), 1280 x 18944 x 3584 53.1 in two rounds of
+// 256 x 192 (58.2 of 256 x 256, 65.2 of 192 x 256, a third round for six tiles), 1 x 12288 x 4096 7.8 (16 x 48) and 11.6 (16 x 16, three rounds).
+// All launches had bf16 results, and the estimate knows no type: float32 results, twice the bytes, take the same plan (12288 x 12288 x 4096 329 us for
+// 297, 1280 x 18944 x 3584 56.7 for 52.6, 512 x 12288 x 4096 21.6 for 20.4).
 struct Mx4Cost { int wide, bm, bn; double start, round, line, w, out, sums, add; };
 constexpr Mx4Cost kMx4Costs[] = {
     {0, 16, 16, 2.44, 1.23, 0.0843, 0.0361, 0.372, 0, 2.5}, {0, 16, 48, 2.1, 1.46, 0.113, 0.0464, 0.698, 0.608, 2.37},

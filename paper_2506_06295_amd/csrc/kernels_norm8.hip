@@ -6,8 +6,8 @@
 // kernel adds them does not reach the codes.  Everything else is float32.  rstd can pass float32's range too (rows of subnormals
 // with eps = 0) and fall below its normal numbers (rows near its largest): then s takes a power of two first and rstd goes without it.
 //
-// Bound by the bytes with many rows: x, stream, sum and codes of 12288 rows of 4096 (bf16, 8 bits) in 70.7 us, 5.0 TB/s; by two trips to memory and a
-// launch with few: 64 rows 4.3 us.
+// Bound by the bytes with many rows: x, stream, sum and codes of 12288 rows of 4096 (bf16, 8 bits) in 70.9 us, 5.0 TB/s; by two trips to memory and a
+// launch with few: 64 rows 4.1 us.  (Times here: the median or best of several means of 20 launches behind one another.)
 #include <cmath>
 
 #include "mx4.hpp"
@@ -201,6 +201,7 @@ __global__ __launch_bounds__(TR) void k_norm_rows(NormRows n, int8_t* __restrict
   }
 }
 
+// Rows over 12288 are read two (4 bits) or three times (8 bits): 4096 x 18944 in bf16 117 and 139 us, their bytes 102 and 110 at 4.95 TB/s.
 // Threads of a row and pieces of a thread by width.  Rows of up to 1024 go to a wavefront each, which waits for nobody (12288 x 256: 10.7 us, 23 with a
 // workgroup of four per row).  2049 to 4096 wide, us for 12288 rows of 4096; 3584; 4049: a bf16 stream 70.7; 57.8; 85 with 256 threads of two pieces and
 // 68.3; 62.5; 95 with 512 of one; a float32 one 105; 97; 116 and 100; 87; 119.  The bytes of 4096 wide take 71 and 112 at 4.95 TB/s, a copy of 4 GB's.
